@@ -35,7 +35,8 @@ extern "C" {
 typedef int32_t asd_dtype;
 enum {
     ASD_F32 = 0,   /* IEEE binary32 */
-    ASD_BF16 = 1   /* bfloat16: the upper 16 bits of a binary32 value */
+    ASD_BF16 = 1,  /* bfloat16: the upper 16 bits of a binary32 value */
+    ASD_F16 = 2    /* IEEE binary16: asd_sample, asd_rope_append and asd_block_attention only */
 };
 
 /* Status of a call (a plain 32-bit integer, like asd_dtype). */
@@ -230,9 +231,14 @@ enum {
     ASD_DEVERR_NEGATIVE_K = 1,   /* a request had K_i < 0 (read as 0) */
     ASD_DEVERR_ROWS = 2,         /* a request's rows lay outside [0, total_rows)
                                     (not verified, or not committed) */
-    ASD_DEVERR_COMMIT = 4        /* a verified request committed nothing: its
+    ASD_DEVERR_COMMIT = 4,       /* a verified request committed nothing: its
                                     tokens did not fit below capacity, seq_len_i
                                     was negative or a_i lay outside [0, K_i] */
+    ASD_DEVERR_CACHE = 8,        /* a request's tokens did not fit its page table, its
+                                    cached length was negative, or a page id lay
+                                    outside the cache */
+    ASD_DEVERR_SAMPLE = 16       /* a logit row had no distribution to sample from (a
+                                    NaN, or every logit -inf) */
 };
 
 /*
@@ -419,6 +425,189 @@ asd_status asd_lmhead_verify(const void *hidden, const void *weight, int64_t d, 
                              const int32_t *exc_cap, asd_budget *budget_inout,
                              int32_t *out_accept_len, int32_t *out_next_token,
                              int32_t *out_argmax, float *out_regret, void *stream);
+
+/*
+ * The operators of a decoding round around the verifier: the block's tokens
+ * enter the target's cache (asd_rope_append), its rows attend to that cache
+ * (asd_block_attention), and tokens are drawn from logit rows (asd_sample: a
+ * drafter's proposals, requests that do not decode greedily).
+ *
+ * The first two share the batch geometry of asd_verify: request i owns the
+ * K_i + 1 rows o_i .. o_i + K_i (block_lens, and row_offsets or the packed
+ * layout), its row p being the token at place cache_len_i + p of its sequence
+ * (with drafts: row 0 is the last committed token, rows 1..K_i the drafts; a
+ * request without drafts has K_i = 0 and one row).  A negative K_i is read as 0
+ * (ASD_DEVERR_NEGATIVE_K); a request whose rows lie outside [0, total_rows)
+ * is skipped (ASD_DEVERR_ROWS), and so is one with cache_len_i < 0 or
+ * cache_len_i + K_i + 1 > max_pages * page_size (ASD_DEVERR_CACHE): none of its
+ * rows, and none of its tokens in the cache, is written.  Rows that no request
+ * owns are left as they were.
+ */
+
+/*
+ * A cache of keys and values in pages.  The token at place t of request i lies
+ * in page page_table[i][t / page_size] at slot t mod page_size; its head h is the
+ * head_dim dense elements from
+ *   page * page_stride + slot * token_stride + h * head_stride
+ * of keys and of values (strides in elements, the same for both), so token-major
+ * and head-major pages, and keys and values interleaved in one array, are all
+ * described.  A page id outside [0, num_pages) sets ASD_DEVERR_CACHE; its tokens
+ * are not written, and are not attended to.
+ */
+typedef struct {
+    void *keys;                 /* 16-byte aligned device memory, dtype elements */
+    void *values;
+    int64_t num_pages;          /* 1 <= num_pages < 2^31 */
+    int64_t page_stride;        /* strides: >= 0, multiples of 8 elements */
+    int64_t token_stride;
+    int64_t head_stride;
+    const int32_t *page_table;  /* int32 [num_requests][max_pages] */
+    int32_t max_pages;          /* 1 <= max_pages; max_pages * page_size < 2^31 */
+    int32_t page_size;          /* tokens a page, >= 1 */
+    int32_t num_heads;          /* heads of keys and values, 1..4096 */
+    int32_t head_dim;           /* D */
+} asd_paged_cache;
+
+/* Flags of asd_rope_append. */
+enum {
+    ASD_ROPE_INTERLEAVED = 1    /* pairs (2j, 2j+1) instead of (j, j + rot_dim/2) */
+};
+
+/*
+ * asd_rope_append -- norms of queries and keys, position rotation and append
+ * of keys and values to the cache, in one pass over a projection's output.
+ *
+ * For every row r of request i and every head of q and k:
+ *   n = x / sqrt(mean(x^2) + eps) * w   (n = x where its norm weight w is NULL)
+ *   y_a = n_a cos - n_b sin, y_b = n_a sin + n_b cos,  angle = pos * inv_freq[j]
+ * for the pairs j < rot_dim / 2, elements from rot_dim on are kept.  The angle
+ * is formed and reduced in binary64, the rest in binary32, and the result is
+ * rounded once to dtype.  Rotated queries go to out_q, rotated keys and the
+ * values to the token's slot of the cache (place cache_len_i + p).
+ *
+ * q, k, v         row r's heads, dense, at q + r * q_stride, k + r * k_stride and
+ *                 v + r * v_stride (strides in elements: three parts of one
+ *                 projection's rows will do).  q may be NULL with out_q NULL
+ *                 and num_q_heads = 0.
+ * dtype           ASD_BF16 or ASD_F16, of q, k, v, the norm weights, out_q and
+ *                 the cache.
+ * num_q_heads     heads of q, 0..4096; k and v have cache->num_heads.
+ * q_norm, k_norm  [head_dim] weights, or NULL: no norm.  eps >= 0, finite.
+ * inv_freq        float [rot_dim / 2]; rot_dim even, 0 <= rot_dim <= head_dim (0: no
+ *                 rotation, inv_freq may be NULL).
+ * flags           0 or ASD_ROPE_INTERLEAVED.
+ * positions       int64 [total_rows], or NULL: pos = cache_len_i + p.  The nodes of
+ *                 a draft tree take their depth: cache_len_i + depth.
+ * cache           head_dim a multiple of 8, 8 <= head_dim <= 256.
+ * num_requests, total_rows, block_lens, row_offsets: as for asd_verify.
+ * cache_lens      int64 [num_requests]: tokens already in the cache (after
+ *                 asd_commit, seq_len - 1: the newest token has no entry yet).
+ * out_q           [total_rows] rows at out_q + r * out_q_stride; may be q itself,
+ *                 with q's stride (each head is read before it is written).
+ * q, k, v, out_q and the norm weights are 16-byte aligned and the strides
+ * multiples of 8.  No other output may alias an input.  Two requests that name
+ * one slot leave either's token there.  Allocates nothing; asynchronous.
+ */
+asd_status asd_rope_append(const void *q, const void *k, const void *v, asd_dtype dtype,
+                           int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                           int32_t num_q_heads, const void *q_norm, const void *k_norm, float eps,
+                           const float *inv_freq, int32_t rot_dim, uint32_t flags,
+                           const int64_t *positions, const asd_paged_cache *cache,
+                           int32_t num_requests, int64_t total_rows, const int32_t *block_lens,
+                           const int64_t *row_offsets, const int64_t *cache_lens, void *out_q,
+                           int64_t out_q_stride, void *stream);
+
+/*
+ * asd_block_attention -- attention of every request's block of rows over its
+ * cache, which holds the block's own tokens already (asd_rope_append).
+ *
+ * Row p, query head h (key head h / (num_q_heads / cache->num_heads)):
+ *   out = sum_t exp(s_t - max s) V_t / sum_t exp(s_t - max s),  s_t = scale q . K_t
+ * over the tokens t < cache_len_i + K_i + 1 that the row sees: every cached one
+ * (t < cache_len_i), and the block's token j = t - cache_len_i where bit j mod 64
+ * of mask[r][j / 64] is set (j >= 64 * mask_words: not seen); with a NULL mask the
+ * tokens j <= p (a chain of drafts).  A row that sees nothing gives zeros.
+ * What hidden tokens hold, infinities and NaN too, does not reach the row.
+ *
+ * Scores, maxima, sums and outputs are held in binary32, the weights enter the
+ * second product rounded to dtype (as the matrix cores take them) and the
+ * output is rounded once.
+ *
+ * q               row r's heads, dense, at q + r * q_stride (elements, a multiple
+ *                 of 8); dtype ASD_BF16 or ASD_F16; 16-byte aligned.
+ * num_q_heads     a positive multiple of cache->num_heads, at most 65,536.
+ * scale           finite.
+ * cache           head_dim 64, 128 or 256.
+ * mask            uint64 [total_rows][mask_words], or NULL with mask_words = 0.
+ * out             [total_rows][num_q_heads][head_dim], dense, 16-byte aligned; no
+ *                 alias of an input.
+ * workspace       NULL: the library workspace of (device, stream), as for
+ *                 asd_verify (allocated on first use, never during capture);
+ *                 otherwise caller memory as for asd_verify_ws, of at least
+ *                 asd_block_attention_workspace_bytes(...) bytes.
+ * Asynchronous on `stream`.
+ */
+asd_status asd_block_attention(const void *q, asd_dtype dtype, int64_t q_stride,
+                               int32_t num_q_heads, float scale, const asd_paged_cache *cache,
+                               int32_t num_requests, int64_t total_rows,
+                               const int32_t *block_lens, const int64_t *row_offsets,
+                               const int64_t *cache_lens, const uint64_t *mask,
+                               int32_t mask_words, void *out, void *stream, void *workspace,
+                               size_t workspace_bytes);
+
+/* Device workspace that asd_block_attention needs for a call of these sizes on
+ * the current device.  0 for sizes it refuses. */
+size_t asd_block_attention_workspace_bytes(int32_t num_q_heads, int32_t num_kv_heads,
+                                           int32_t head_dim, int32_t num_requests,
+                                           int64_t total_rows);
+
+/*
+ * asd_sample -- draw one token from every logit row.
+ *
+ * With w_v = exp((z_v - max z) / T), the tokens ranked by logit (greatest first,
+ * the lower index first among equals), a row keeps the shortest of these
+ * prefixes of the ranking:
+ *   top-k   the first k tokens (k <= 0: all);
+ *   top-p   the fewest tokens whose weights sum to at least p times the weights
+ *           of the first k (p >= 1 or NaN: all of them; at least one);
+ *   min-p   the tokens with w_v >= min_p (min_p <= 0 or NaN: all; min_p > 1 is
+ *           read as 1), so in effect p_v >= min_p p_max;
+ * and the token drawn is the first, by index, at which the running sum of the
+ * kept weights exceeds u times their sum.  T <= 0 or NaN: the row's argmax
+ * (lowest index among equals), whatever k, p, min_p and u are.  Weights are
+ * held to 2^-44 of the greatest or better and summed without further rounding,
+ * so the same row gives the same token in any batch.
+ *
+ * -0 equals +0; a logit of -inf has no weight; where the greatest is +inf the
+ * tokens at +inf share the weight.  A row that holds a NaN, or nothing but -inf,
+ * has no distribution: its token is -1, its probability 0, and
+ * ASD_DEVERR_SAMPLE is set.  u outside [0, 1) is read as the nearest value
+ * inside, NaN as 0.
+ *
+ * logits          row r's vocab elements, dense, at logits + r * row_stride
+ *                 (elements, row_stride >= vocab: rows may be padded); the base
+ *                 address a multiple of the element size.
+ * dtype           ASD_F32, ASD_BF16 or ASD_F16.
+ * vocab           1 <= vocab < 2^30;  rows: 0 <= rows < 2^31 (0 returns ASD_OK).
+ * temperature     float [rows], or NULL: T = 1.
+ * top_k           int32 [rows], or NULL: all.
+ * top_p, min_p    float [rows], or NULL: all.
+ * uniform         float [rows]: u, uniform on [0, 1).
+ * out_token       int32 [rows].
+ * out_prob        float [rows] or NULL: the drawn token's share of the kept
+ *                 weights (1 for an argmax).
+ * workspace       as for asd_block_attention, asd_sample_workspace_bytes(...).
+ * Asynchronous on `stream`.
+ */
+asd_status asd_sample(const void *logits, asd_dtype dtype, int64_t vocab, int64_t rows,
+                      int64_t row_stride, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, const float *uniform,
+                      int32_t *out_token, float *out_prob, void *stream, void *workspace,
+                      size_t workspace_bytes);
+
+/* Device workspace that asd_sample needs for a call of these sizes on the
+ * current device.  0 for sizes it refuses. */
+size_t asd_sample_workspace_bytes(asd_dtype dtype, int64_t vocab, int64_t rows);
 
 /*
  * asd_row_splits -- the number S of column tiles per row that asd_verify cuts

@@ -21,22 +21,27 @@ import warnings
 
 import torch
 
-from .build import BINDING, HASHED_SOURCES, LIBRARY, binding_hash, source_hash
+from .build import BINDING, DECODE_HEADERS, DECODE_SOURCES, HASHED_SOURCES, LIBRARY, binding_hash, source_hash
 
 __all__ = ["asd_verify", "asd_verify_static", "asd_verify_ws", "asd_verify_ex", "asd_shard_argmax",
            "asd_verify_partials", "asd_opportunity", "asd_commit", "asd_verify_commit",
-           "asd_lmhead_verify", "asd_device_error", "asd_row_splits", "asd_row_pass", "asd_read_probe",
+           "asd_lmhead_verify", "asd_rope_append", "asd_block_attention", "asd_sample",
+           "asd_block_attention_workspace_bytes", "asd_sample_workspace_bytes", "asd_device_error", "asd_row_splits", "asd_row_pass", "asd_read_probe",
            "asd_mfma_probe", "asd_workspace_bytes",
-           "asd_status_string", "asd_version", "asd_release", "AsdError", "ASD_F32", "ASD_BF16",
+           "asd_status_string", "asd_version", "asd_release", "AsdError", "ASD_F32", "ASD_BF16", "ASD_F16",
            "ASD_GATE_RAW", "ASD_DEVERR_NEGATIVE_K", "ASD_DEVERR_ROWS", "ASD_DEVERR_COMMIT",
+           "ASD_DEVERR_CACHE", "ASD_DEVERR_SAMPLE",
            "library_path", "library_source_hash", "check_built_from_sources"]
 
 ASD_F32 = 0
 ASD_BF16 = 1
+ASD_F16 = 2                 # the decoding operators only
 ASD_GATE_RAW = 1            # asd_verify_ex flag: gate on r <= g instead of r / q <= g
 ASD_DEVERR_NEGATIVE_K = 1   # device error word bits (asd_device_error)
 ASD_DEVERR_ROWS = 2
 ASD_DEVERR_COMMIT = 4
+ASD_DEVERR_CACHE = 8
+ASD_DEVERR_SAMPLE = 16
 ASD_ESCRATCH = 6            # status: the call needs more than asd_verify_static's scratch
 ASD_STATIC_SCRATCH_BYTES = 4 << 20
 _DTYPES = {torch.float32: ASD_F32, torch.bfloat16: ASD_BF16}
@@ -63,7 +68,7 @@ def library_source_hash(lib) -> str:
 def check_built_from_sources(lib, path=LIBRARY):
     """Raise unless the library was built from the sources beside it (the hash
     embedded by the build equals the hash of the current sources)."""
-    if not all(os.path.exists(p) for p in HASHED_SOURCES):
+    if not all(os.path.exists(p) for p in HASHED_SOURCES + DECODE_SOURCES + DECODE_HEADERS):
         raise RuntimeError("the sources of %s are missing; cannot check the build" % path)
     built, current = library_source_hash(lib), source_hash()
     if built != current:
@@ -117,6 +122,20 @@ def _load():
     lib.asd_verify_commit.argtypes = common[:-1] + [vp, i64, vp, vp, vp, vp, sz]
     lib.asd_verify_commit.restype = ctypes.c_int
     lib.asd_commit.restype = ctypes.c_int
+    u32, f32 = ctypes.c_uint32, ctypes.c_float
+    lib.asd_rope_append.argtypes = [vp, vp, vp, ctypes.c_int, i64, i64, i64, i32, vp, vp, f32, vp,
+                                    i32, u32, vp, vp, i32, i64, vp, vp, vp, vp, i64, vp]
+    lib.asd_rope_append.restype = ctypes.c_int
+    lib.asd_block_attention.argtypes = [vp, ctypes.c_int, i64, i32, f32, vp, i32, i64, vp, vp, vp,
+                                        vp, i32, vp, vp, vp, sz]
+    lib.asd_block_attention.restype = ctypes.c_int
+    lib.asd_block_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
+    lib.asd_block_attention_workspace_bytes.restype = sz
+    lib.asd_sample.argtypes = [vp, ctypes.c_int, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                               sz]
+    lib.asd_sample.restype = ctypes.c_int
+    lib.asd_sample_workspace_bytes.argtypes = [ctypes.c_int, i64, i64]
+    lib.asd_sample_workspace_bytes.restype = sz
     lib.asd_workspace_bytes.argtypes = [ctypes.c_int, i64, i32, i64]
     lib.asd_workspace_bytes.restype = sz
     lib.asd_status_string.argtypes = [ctypes.c_int]
@@ -710,3 +729,7 @@ def asd_lmhead_verify(hidden, weight, draft_tokens, block_lens, tau, exc_cap, bu
     if st != 0:
         raise AsdError(st, "asd_lmhead_verify")
     return acc, nxt
+
+
+from .decode import (asd_block_attention, asd_block_attention_workspace_bytes,  # noqa: E402
+                     asd_rope_append, asd_sample, asd_sample_workspace_bytes)

@@ -8,18 +8,25 @@ The build embeds a hash of the sources it compiled in ``asd_version()``; the
 binding refuses a library whose hash differs from the sources beside it, so a
 stale build is never tested, benchmarked or smoke-checked by mistake.
 """
+import concurrent.futures
 import hashlib
 import os
 import re
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIBRARY = os.path.join(HERE, "libasd.so")
-SOURCES = [os.path.join(CSRC, "asd_api.cpp"), os.path.join(CSRC, "asd_kernels.hip")]
-# Every file whose code goes into the library (sources and headers).
+# The decoding operators around the verifier, and the header they share.
+DECODE_SOURCES = [os.path.join(CSRC, "asd_decode_api.cpp"), os.path.join(CSRC, "asd_cache.hip"),
+                  os.path.join(CSRC, "asd_sample.hip")]
+DECODE_HEADERS = [os.path.join(CSRC, "asd_decode.h")]
+SOURCES = [os.path.join(CSRC, "asd_api.cpp"), os.path.join(CSRC, "asd_kernels.hip"), *DECODE_SOURCES]
+# The verifier's sources and headers; with DECODE_SOURCES and DECODE_HEADERS, every file whose
+# code goes into the library.
 HASHED_SOURCES = [os.path.join(CSRC, "asd_kernels.hip"), os.path.join(CSRC, "asd_plan.h"),
                   os.path.join(CSRC, "asd_api.cpp"), os.path.join(ROOT, "include", "asd.h")]
 # The binding's native marshalling (a CPython module over torch's C++ tensors).
@@ -39,7 +46,7 @@ def source_hash(paths=None) -> str:
     whitespace removed: an edit to a comment keeps the hash, any code edit
     changes it."""
     h = hashlib.sha256()
-    for p in (HASHED_SOURCES if paths is None else paths):
+    for p in (HASHED_SOURCES + DECODE_SOURCES + DECODE_HEADERS if paths is None else paths):
         with open(p) as f:
             text = f.read()
         text = re.sub(r"/\*.*?\*/", " ", text, flags=re.S)
@@ -50,10 +57,21 @@ def source_hash(paths=None) -> str:
 
 def build_library(verbose: bool = False, output: str = LIBRARY, extra_flags=()) -> str:
     tag = '-DASD_SOURCE_HASH="%s"' % source_hash()
-    cmd = [HIPCC, *HIP_FLAGS, tag, *extra_flags, "-shared", *SOURCES, "-o", output + ".tmp"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.run(cmd, check=True)
+    with tempfile.TemporaryDirectory() as objects, \
+            concurrent.futures.ThreadPoolExecutor(len(SOURCES)) as pool:
+        def compile_one(source):
+            obj = os.path.join(objects, os.path.basename(source) + ".o")
+            cmd = [HIPCC, *HIP_FLAGS, tag, *extra_flags, "-c", source, "-o", obj]
+            if verbose:
+                print(" ".join(cmd), flush=True)
+            subprocess.run(cmd, check=True)
+            return obj
+
+        link = [HIPCC, "--offload-arch=gfx950", "-shared", *pool.map(compile_one, SOURCES), "-o",
+                output + ".tmp"]
+        if verbose:
+            print(" ".join(link), flush=True)
+        subprocess.run(link, check=True)
     os.replace(output + ".tmp", output)
     return output
 

@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "../../include/asd.h"
+#include "asd_decode.h"
 #include "asd_plan.h"
 
 namespace asd {
@@ -244,7 +245,37 @@ asd_status resolve_workspace(hipStream_t s, const Plan& plan, void* workspace,
     return library_workspace(s, plan.ws_bytes, out, counter);
 }
 
+// The current device's error word, looked up once per device.
+asd_status error_word(uint32_t** out) {
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return ASD_EHIP;
+    std::lock_guard<std::mutex> lock(g_mutex);
+    auto it = g_error_words.find(device);
+    if (it != g_error_words.end()) {
+        *out = it->second;
+        return ASD_OK;
+    }
+    uint32_t* word = nullptr;
+    if (error_word_address(&word) != hipSuccess || !word) return ASD_EHIP;
+    g_error_words[device] = *out = word;
+    return ASD_OK;
+}
+
 }  // namespace
+
+asd_status decode_workspace(hipStream_t stream, size_t bytes, void** out) {
+    return library_workspace(stream, bytes, out);
+}
+
+asd_status decode_compute_units(int* out) {
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return ASD_EHIP;
+    std::lock_guard<std::mutex> lock(g_mutex);
+    return cu_count(device, out);
+}
+
+asd_status decode_error_word(uint32_t** out) { return error_word(out); }
+
 }  // namespace asd
 
 using namespace asd;
@@ -361,19 +392,9 @@ asd_status asd_device_error(uint32_t* out_word, int32_t clear, void* stream) {
     hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing(s, &cap) != hipSuccess) return ASD_EHIP;
     if (cap != hipStreamCaptureStatusNone) return ASD_ECAPTURE;
-    int device = 0;
-    if (hipGetDevice(&device) != hipSuccess) return ASD_EHIP;
     uint32_t* word = nullptr;
-    {
-        std::lock_guard<std::mutex> lock(g_mutex);
-        auto it = g_error_words.find(device);
-        if (it == g_error_words.end()) {
-            if (error_word_address(&word) != hipSuccess || !word) return ASD_EHIP;
-            g_error_words[device] = word;
-        } else {
-            word = it->second;
-        }
-    }
+    const asd_status st = error_word(&word);
+    if (st != ASD_OK) return st;
     uint32_t host = 0;
     if (hipMemcpyAsync(&host, word, sizeof host, hipMemcpyDeviceToHost, s) != hipSuccess)
         return ASD_EHIP;

@@ -1,0 +1,182 @@
+"""asd_sample against its 64-bit form: tokens equal, probabilities to a rounding."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_03447_amd as asd
+from oracle import decode
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+def check(logits, u, t=None, k=None, p=None, m=None, **kw):
+    rows = logits.shape[0]
+    prob = torch.full((rows,), 7.0, device=DEV)
+
+    def dev(x, dtype):
+        return None if x is None else torch.tensor(x, dtype=dtype).expand(rows).contiguous().to(DEV)
+
+    u = torch.as_tensor(u, dtype=torch.float32).to(DEV).expand(rows).contiguous()
+    args = [dev(t, torch.float32), dev(k, torch.int32), dev(p, torch.float32), dev(m, torch.float32)]
+    token = asd.asd_sample(logits, u, temperature=args[0], top_k=args[1], top_p=args[2],
+                           min_p=args[3], out_prob=prob, **kw)
+    torch.cuda.synchronize()
+    z = logits.float().cpu().numpy()
+    a = [[d] * rows if x is None else x.cpu().double().tolist() for x, d in zip(args, (1.0, 0, 1.0, 0.0))]
+    uu = u.cpu().double().tolist()
+    want = [decode.sample_row(z[r], uu[r], *(x[r] for x in a)) for r in range(rows)]
+    assert token.cpu().tolist() == [w[0] for w in want]
+    exact = np.array([w[1] for w in want])
+    # one rounding to binary32, the weights' 2^-44
+    assert (np.abs(prob.cpu().double().numpy() - exact) <= exact * 2.0 ** -23 + 2.0 ** -40).all()
+    return token
+
+
+def rows_of(rows, vocab, dtype, seed, sigma=2.0, pad=0):
+    gen = torch.Generator().manual_seed(seed)
+    z = sigma * torch.randn((rows, vocab + pad), generator=gen)
+    likely = torch.randint(vocab, (rows, 8), generator=gen)
+    z.scatter_add_(1, likely, 10 * torch.rand((rows, 1), generator=gen).expand(rows, 8))
+    return z.to(dtype).to(DEV)[:, :vocab], torch.rand(rows, generator=gen)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab,pad", [(1, 0), (2, 1), (63, 0), (64, 3), (257, 0), (1000, 24),
+                                       (4097, 1), (32000, 0), (50257, 7), (151936, 0)])
+def test_every_filter_over_the_sizes(dtype, vocab, pad):
+    rows = 12
+    z, u = rows_of(rows, vocab, dtype, vocab + pad, pad=pad)
+    check(z, u)
+    check(z, u, t=0.7)
+    check(z, u, k=[0, 1, 2, 3, 5, 20, 50, 100, 1000, 5000, 1 << 30, -1])
+    check(z, u, p=[1.0, 0.99, 0.95, 0.9, 0.8, 0.7, 0.5, 0.3, 0.1, 0.0, -1.0, 2.0])
+    check(z, u, m=[0.0, 1.0, 0.9, 0.5, 0.3, 0.1, 0.05, 0.02, 0.01, 1e-4, 1e-9, 2.0])
+    check(z, u, t=[0.8, 1.2, 0.3, 1.0] * 3, k=[50, 0, 7, 300] * 3, p=[0.95, 0.9, 1.0, 0.6] * 3,
+          m=[0.0, 0.05, 0.01, 0.0] * 3)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_flat_rows_keep_many_tokens(dtype):
+    """The nucleus of a flat row is most of the vocabulary, with long ties in 16 bits."""
+    gen = torch.Generator().manual_seed(5)
+    z = (0.5 * torch.randn((16, 60001), generator=gen)).to(dtype).to(DEV)
+    u = torch.linspace(0, 0.999, 16)
+    check(z, u)
+    check(z, u, p=[0.9, 0.5, 0.99, 0.05] * 4)
+    check(z, u, k=[30000, 10, 60000, 9999] * 4, p=[0.9, 0.5, 0.99, 0.05] * 4)
+    check(z, u, m=[0.5, 0.01, 0.9, 0.2] * 4, t=[1.0, 2.0, 0.1, 100.0] * 4)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [8, 1024, 40960])
+def test_ties_go_to_the_lowest_index_and_edges_are_exact(dtype, vocab):
+    """Equal logits: every running sum is a whole number, so u and p on an edge are exact."""
+    z = torch.zeros((8, vocab), dtype=dtype, device=DEV)
+    u = torch.arange(8) / 8.0
+    assert check(z, u).tolist() == [vocab * j // 8 for j in range(8)]
+    assert check(z, u, p=0.5).tolist() == [vocab * j // 16 for j in range(8)]
+    assert check(z, u, k=8).tolist() == list(range(8))
+    assert check(z, u, k=8, p=0.25).tolist() == [j // 4 for j in range(8)]
+    z[:, 1::2] = -3.0
+    assert check(z, u, m=0.5).tolist() == [2 * (vocab // 2 * j // 8) for j in range(8)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_of_unusual_values(dtype):
+    lowest, big = torch.finfo(dtype).min, torch.finfo(dtype).max
+    inf, nan = math.inf, math.nan
+    rows = [[nan, 0, 0, 0], [0, 1, 2, nan], [-inf] * 4, [inf, 0, inf, -inf], [inf, nan, 0, 0],
+            [lowest] * 4, [lowest, 0, lowest, lowest], [big, lowest, 0, big], [-inf, -inf, lowest, -inf],
+            [-0.0, 0.0, -0.0, 0.0], [-inf, 5, -inf, 5], [-nan, 0, 0, 0]]
+    z = torch.tensor(rows, dtype=torch.float64).to(dtype).to(DEV)
+    asd.asd_device_error(clear=True)
+    for u in (0.0, 0.4, 0.6, 0.999999):
+        for t in (None, 0.0, 1e-30, 1e30, inf, nan, -1.0, 1e-45):
+            check(z, u, t=t)
+        check(z, u, k=2)
+        check(z, u, p=0.6)
+        check(z, u, m=0.5)
+        check(z, u, k=3, p=0.9, m=0.1)
+        check(z, u, p=nan, m=nan)
+    assert asd.asd_device_error(clear=True) == asd.ASD_DEVERR_SAMPLE
+    check(z[9:11], 0.5)
+    assert asd.asd_device_error(clear=True) == 0
+
+
+def test_u_outside_its_range():
+    z, _ = rows_of(6, 1000, torch.float32, 3)
+    check(z, torch.tensor([-1.0, 0.0, 1.0, 2.0, math.inf, math.nan]), t=0.9)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_at_any_address_and_apart(dtype):
+    base = torch.zeros(64 + 7 * 1303, dtype=dtype, device=DEV)
+    for start in (0, 1, 2, 3, 5, 7):
+        for stride in (1300, 1301, 1303):
+            z, u = rows_of(5, 1300, dtype, start + stride)
+            view = base[start:start + 5 * stride].as_strided((5, 1300), (stride, 1))
+            view.copy_(z)
+            check(view, u, t=0.9, k=40, p=0.9)
+            check(view, u, p=0.95)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_row_draws_the_same_in_any_batch(dtype):
+    z, u = rows_of(300, 20011, dtype, 11, sigma=1.0)
+    u = u.to(DEV)
+    p = torch.rand(300).to(DEV)
+    whole = asd.asd_sample(z, u, top_p=p, temperature=1.1)
+    for a, b in ((0, 1), (17, 20), (100, 300)):
+        part = asd.asd_sample(z[a:b], u[a:b], top_p=p[a:b].contiguous(), temperature=1.1)
+        assert torch.equal(part, whole[a:b])
+
+
+def test_draws_follow_the_distribution():
+    z = torch.tensor([0.0, 1.0, 2.0, 3.0, -1.0], device=DEV).expand(20000, 5).contiguous()
+    u = (torch.arange(20000, device=DEV) + 0.5) / 20000
+    token = asd.asd_sample(z, u, temperature=0.9)
+    share = torch.bincount(token.long(), minlength=5).double() / 20000
+    # evenly spaced u: each token's share to the one draw at either edge
+    assert ((share - torch.softmax(z[0].double() / 0.9, 0)).abs() <= 1.0 / 20000).all()
+
+
+def test_other_streams_graphs_and_workspaces():
+    z, u = rows_of(40, 50001, torch.bfloat16, 2)
+    u = u.to(DEV)
+    want = asd.asd_sample(z, u, top_p=0.9)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    size = max(1, asd.asd_sample_workspace_bytes(torch.bfloat16, 50001, 40))
+    space = torch.empty(size, dtype=torch.uint8, device=DEV)
+    with torch.cuda.stream(side):
+        assert torch.equal(asd.asd_sample(z, u, top_p=0.9), want)
+        p = torch.full((40,), 0.9, device=DEV)
+        out = torch.zeros(40, dtype=torch.int32, device=DEV)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            asd.asd_sample(z, u, top_p=p, out_token=out, workspace=space)
+    torch.cuda.synchronize()
+    for turn in range(4):
+        zz, uu = rows_of(40, 50001, torch.bfloat16, 100 + turn)
+        z.copy_(zz)
+        u.copy_(uu)
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = out.clone()
+        assert torch.equal(asd.asd_sample(z, u, top_p=p), replayed)
+
+
+def test_empty_and_scalar_arguments():
+    z, u = rows_of(4, 100, torch.float32, 1)
+    u = u.to(DEV)
+    assert asd.asd_sample(z[:0], u[:0]).shape == (0,)
+    a = asd.asd_sample(z, u, temperature=0.5, top_k=10, top_p=0.9, min_p=0.01)
+    full = [torch.full((4,), x, dtype=d, device=DEV) for x, d in
+            ((0.5, torch.float32), (10, torch.int32), (0.9, torch.float32), (0.01, torch.float32))]
+    b = asd.asd_sample(z, u, temperature=full[0], top_k=full[1], top_p=full[2], min_p=full[3])
+    assert torch.equal(a, b)
