@@ -1,5 +1,4 @@
-// gfx950 kernels of the paged cache: norms, rotation and append of a block's
-// rows, and the attention of the block to the cache.
+// gfx950 kernel of the paged cache: norms, rotation and append of a block's rows.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -12,12 +11,6 @@ namespace {
 
 __device__ __forceinline__ float widen(__bf16 x) { return (float)x; }
 __device__ __forceinline__ float widen(_Float16 x) { return (float)x; }
-
-// LDS written by one lane of a wavefront is read by another after this.
-__device__ __forceinline__ void wave_sync() {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-}
 
 // ------------------------------------------------------------ geometry
 
@@ -129,71 +122,6 @@ __global__ __launch_bounds__(kAppendThreads) void asd_rope_append_kernel(RopeApp
     }
 }
 
-// ------------------------------------------------------------ attention
-
-// One wavefront per (row, query head): 64 tokens at a time, a lane scores its token, then the lanes share out the head's elements.
-template <typename T>
-__global__ __launch_bounds__(64) void asd_block_attention_kernel(AttentionArgs a) {
-    __shared__ float q[256];
-    const int lane = threadIdx.x;
-    const int32_t i = (int32_t)blockIdx.x;
-    const Request r = request_of(a.b, i, lane);
-    if (!r.ok) return;
-    const int d = a.b.cache.head_dim, h = (int)blockIdx.z;
-    const int kvh = h / (a.num_q_heads / a.b.cache.num_heads);
-    const int64_t total = r.cached + r.count, head = (int64_t)kvh * a.b.cache.head_stride;
-    for (int32_t p = (int32_t)blockIdx.y; p < r.count; p += (int32_t)gridDim.y) {
-        const int64_t row = r.row + p;
-        const T* src = (const T*)a.q + row * a.q_stride + (int64_t)h * d;
-        __syncthreads();
-        for (int e = lane; e < d; e += 64) q[e] = widen(src[e]) * a.scale;
-        __syncthreads();
-        float best = -INFINITY, sum = 0.0f, o[4] = {0, 0, 0, 0};
-        for (int64_t t0 = 0; t0 < total; t0 += 64) {
-            const int64_t t = t0 + lane;
-            int64_t slot = -1;
-            if (t < total) slot = slot_of(a.b, i, t);
-            bool seen = slot >= 0;
-            if (seen && t >= r.cached) {
-                const int64_t j = t - r.cached;
-                seen = a.mask ? j < 64 * (int64_t)a.mask_words &&
-                                    ((a.mask[row * a.mask_words + j / 64] >> (j % 64)) & 1) != 0
-                              : j <= p;
-            }
-            float s = -INFINITY;
-            if (seen) {
-                const T* key = (const T*)a.b.cache.keys + slot + head;
-                s = 0.0f;
-                for (int e = 0; e < d; ++e) s = fmaf(q[e], widen(key[e]), s);
-            }
-            float m = s;
-            bool nan = s != s;
-            for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-            if (__ballot(nan)) m = NAN;
-            const float top = best > m ? best : m;
-            if (top == -INFINITY) continue;
-            const float keep = expf(best - top), w = seen ? expf(s - top) : 0.0f;
-            best = top;
-            sum *= keep;
-            for (int e = 0; e < 4; ++e) o[e] *= keep;
-            float add = w;
-            for (int x = 32; x > 0; x >>= 1) add += __shfl_xor(add, x);
-            sum += add;
-            for (int x = 0; x < 64; ++x) {
-                if (!__shfl((int)seen, x)) continue;
-                const float wx = __shfl(w, x);
-                const int64_t sx = __shfl((long long)slot, x);
-                const T* value = (const T*)a.b.cache.values + sx + head;
-                for (int e = 0; e * 64 + lane < d; ++e)
-                    o[e] = fmaf(wx, widen(value[e * 64 + lane]), o[e]);
-            }
-        }
-        T* dst = (T*)a.out + (row * a.num_q_heads + h) * d;
-        for (int e = 0; e * 64 + lane < d; ++e)
-            dst[e * 64 + lane] = (T)(best == -INFINITY ? 0.0f : o[e] / sum);
-    }
-}
-
 // Workgroups per request: its share of the rows, the batch's requests of any length.
 unsigned rows_share(const Blocks& b) {
     const int64_t y = (b.total_rows + b.num_requests - 1) / b.num_requests;
@@ -208,17 +136,6 @@ hipError_t launch_rope_append(const RopeAppendArgs& a, bool bf16, hipStream_t st
         asd_rope_append_kernel<__bf16><<<grid, kAppendThreads, 0, stream>>>(a);
     else
         asd_rope_append_kernel<_Float16><<<grid, kAppendThreads, 0, stream>>>(a);
-    return hipGetLastError();
-}
-
-size_t attention_workspace_bytes(int32_t, int32_t, int32_t, int32_t, int64_t, int) { return 0; }
-
-hipError_t launch_block_attention(const AttentionArgs& a, bool bf16, void*, int, hipStream_t stream) {
-    const dim3 grid((unsigned)a.b.num_requests, rows_share(a.b), (unsigned)a.num_q_heads);
-    if (bf16)
-        asd_block_attention_kernel<__bf16><<<grid, 64, 0, stream>>>(a);
-    else
-        asd_block_attention_kernel<_Float16><<<grid, 64, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -32,6 +32,14 @@ struct Blocks {
     uint32_t* error_word;
 };
 
+#ifdef __HIPCC__
+// LDS written by one lane of a wavefront is read by another after this.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+#endif
+
 struct RopeAppendArgs {
     Blocks b;
     const void *q, *k, *v;

@@ -1,5 +1,6 @@
 // C ABI of the decoding operators: host-side argument checks and workspaces.
-// Their kernels are in asd_cache.hip (append and attention) and asd_sample.hip.
+// Their kernels are in asd_cache.hip (append), asd_attend.hip (attention) and
+// asd_sample.hip.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
