@@ -23,27 +23,46 @@ constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / 64;
 constexpr int kStrip = 32;                          // tokens a wavefront takes at a time
 constexpr int kUnit = kStrip * kAttendWaves;
 
-// Where stretch x of the batch's `total` units begins: floor(total x / wgs).
-__device__ __forceinline__ int64_t bound_of(int64_t total, int64_t wgs, int64_t x) {
-    const int64_t q = total / wgs;
-    return q * x + (total - q * wgs) * x / wgs;
+// The same value in every lane, in scalar registers.
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+    return (int64_t)((uint64_t)(uint32_t)uniform((int32_t)x) | (uint64_t)(uint32_t)uniform((int32_t)(x >> 32)) << 32);
 }
 
+// The same value, as the compiler sees it a new one: what is computed from it is not kept in registers
+// from before the point where it is taken.
+__device__ __forceinline__ int32_t fresh(int32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// floor(a / b) of uniform 0 <= a < 2^53 and b > 0: a quotient in binary64, put right by one step at most.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    int64_t q = (int64_t)((double)a * (1.0 / (double)b));
+    q -= q * b > a;
+    return uniform(q + ((q + 1) * b <= a));
+}
+
+// Where a workgroup's stretch begins.
 struct Where {
+    int64_t id;         // the stretch, -1: there is none for this workgroup
+    int64_t per;        // units a stretch; the last one may have fewer
     int64_t total;      // units of the batch
-    int64_t unit;       // the unit asked for, counted within its request
-    int64_t row;        // the request's first row
-    int32_t request;    // -1: the unit lies behind the last one
+    int64_t unit;       // the stretch's first unit, counted within its request
+    int64_t row;        // that request's first row
+    int64_t cached;
+    int32_t request, count;
 };
 
-__device__ __forceinline__ int64_t units_of(const Blocks& b, int32_t group, int32_t rows, int64_t row,
-                                            int32_t count, int64_t cached, uint32_t& err) {
+template <int kRows>
+__device__ __forceinline__ int64_t units_of(const Blocks& b, int32_t group, int64_t row, int32_t count,
+                                            int64_t cached, uint32_t& err) {
     const int64_t room = (int64_t)b.cache.max_pages * b.cache.page_size;
     const bool rows_ok = row >= 0 && row <= b.total_rows - count;
     const bool cache_ok = cached >= 0 && cached <= room - count;
     err |= (rows_ok ? 0u : kDecodeErrRows) | (cache_ok ? 0u : kDecodeErrCache);
     if (!rows_ok || !cache_ok) return 0;
-    const int64_t tiles = ((int64_t)count * group + rows - 1) / rows;
+    const int64_t tiles = ((int64_t)count * group + kRows - 1) / kRows;
     return tiles * b.cache.num_heads * ((cached + count + kUnit - 1) / kUnit);
 }
 
@@ -51,6 +70,7 @@ __device__ __forceinline__ int64_t units_of(const Blocks& b, int32_t group, int3
 __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* box, int64_t* total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     long long sum = v;
+#pragma unroll
     for (int s = 1; s < 64; s <<= 1) {
         const long long up = __shfl_up(sum, s);
         if (lane >= s) sum += up;
@@ -59,6 +79,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* box, int64_t* 
     if (lane == 63) box[wave] = sum;
     __syncthreads();
     int64_t before = 0, all = 0;
+#pragma unroll
     for (int w = 0; w < kAttendWaves; ++w) {
         before += w < wave ? box[w] : 0;
         all += box[w];
@@ -67,38 +88,45 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* box, int64_t* 
     return before + sum - v;
 }
 
-// The unit at which stretch `id` of `wgs` begins, found by the whole workgroup.
-__device__ Where locate(const Blocks& b, int32_t group, int32_t rows, int64_t id, int64_t wgs,
-                        bool report, int64_t* box, Where* out) {
-    const int32_t n = b.num_requests, per = (n + kAttendThreads - 1) / kAttendThreads;
-    const int32_t first = min(n, (int32_t)threadIdx.x * per), last = min(n, first + per);
-    int64_t row = 0, unused;
+// The workgroup's stretch: every thread sums its share of the requests (one, up to 256 requests),
+// and the one whose share holds the stretch's first unit says where it is.
+template <int kRows>
+__device__ __forceinline__ Where locate(const Blocks& b, int32_t group, int64_t* box, Where* out) {
+    const int32_t n = b.num_requests, per_thread = (n + kAttendThreads - 1) / kAttendThreads;
+    const int32_t first = min(n, (int32_t)threadIdx.x * per_thread), last = min(n, first + per_thread);
+    int64_t row = 0, unused, mine = 0;
     uint32_t err = 0;
+    const int32_t k0 = first < last ? b.block_lens[first] : 0;
+    const int64_t c0 = first < last ? b.cache_lens[first] : 0;
     if (!b.row_offsets) {
-        int64_t mine = 0;
-        for (int32_t i = first; i < last; ++i) mine += max(b.block_lens[i], 0) + 1;
+        for (int32_t i = first; i < last; ++i) mine += rows_of_block(i == first ? k0 : b.block_lens[i]);
         row = block_scan(mine, box, &unused);
     }
     int64_t units = 0, at = row;
     for (int32_t i = first; i < last; ++i) {
-        const int32_t k = b.block_lens[i], count = max(k, 0) + 1;
+        const int32_t k = i == first ? k0 : b.block_lens[i], count = rows_of_block(k);
         err |= k < 0 ? kDecodeErrNegativeK : 0u;
-        units += units_of(b, group, rows, b.row_offsets ? b.row_offsets[i] : at, count, b.cache_lens[i], err);
+        units += units_of<kRows>(b, group, b.row_offsets ? b.row_offsets[i] : at, count,
+                                 i == first ? c0 : b.cache_lens[i], err);
         at += count;
     }
-    if (report && err != 0) atomicOr(b.error_word, err);
+    if (blockIdx.x == 0 && err != 0) atomicOr(b.error_word, err);
     int64_t total;
     int64_t before = block_scan(units, box, &total);
-    const int64_t unit = bound_of(total, wgs, id);
-    if (threadIdx.x == 0) *out = Where{total, 0, 0, -1};
-    __syncthreads();
+    // Equal stretches, the last one short.  Workgroups go to the XCDs in turn; neighbouring
+    // stretches, which may share keys and values, go to one of them.
+    const int64_t wgs = gridDim.x, per = total <= wgs ? 1 : quotient(total + wgs - 1, wgs);
+    const int64_t used = per == 1 ? total : quotient(total + per - 1, per), eighth = (used + 7) / 8;
+    const int64_t id = (int64_t)(blockIdx.x & 7) * eighth + (blockIdx.x >> 3), unit = id * per;
+    if ((int64_t)(blockIdx.x >> 3) >= eighth || id >= used) return Where{-1, 0, 0, 0, 0, 0, 0, 0};
     if (unit >= before && unit < before + units) {
         for (int32_t i = first; i < last; ++i) {
-            const int32_t count = max(b.block_lens[i], 0) + 1;
+            const int32_t count = rows_of_block(i == first ? k0 : b.block_lens[i]);
+            const int64_t cached = i == first ? c0 : b.cache_lens[i];
             const int64_t at_row = b.row_offsets ? b.row_offsets[i] : row;
-            const int64_t u = units_of(b, group, rows, at_row, count, b.cache_lens[i], err);
+            const int64_t u = units_of<kRows>(b, group, at_row, count, cached, err);
             if (unit < before + u) {
-                *out = Where{total, unit - before, at_row, i};
+                *out = Where{id, per, total, unit - before, at_row, cached, i, count};
                 break;
             }
             before += u;
@@ -106,8 +134,18 @@ __device__ Where locate(const Blocks& b, int32_t group, int32_t rows, int64_t id
         }
     }
     __syncthreads();
-    return *out;
+    return Where{uniform(out->id),  uniform(out->per),    uniform(out->total),   uniform(out->unit),
+                 uniform(out->row), uniform(out->cached), uniform(out->request), uniform(out->count)};
 }
+
+// The item that the end of a workgroup's stretch cuts, if that stretch is its first: every
+// workgroup writes one, those without a stretch too, since nothing else clears them.
+struct alignas(32) Cut {
+    int64_t row;        // the request's first row
+    int32_t id;         // the stretch
+    int32_t head, first, pairs;
+    int32_t parts;      // stretches that hold a part of the item, 0: it is not cut here
+};
 
 template <typename T> struct Half;
 template <> struct Half<__bf16> {
@@ -126,6 +164,9 @@ template <> struct Half<_Float16> {
     }
     static constexpr uint32_t kExponent = 0x7c00u;
 };
+
+// Workgroups that fit on a compute unit, by their registers.
+constexpr int resident(int head_dim, int tiles) { return head_dim == 256 ? 1 : tiles == 1 ? 3 : 2; }
 
 // The greatest / the sum over the four lanes that hold one query row (lanes l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float rows_max(float x) {
@@ -158,7 +199,8 @@ constexpr float kLead = 14.0f, kSet = 6.0f;
 // v_perm: nothing goes through LDS but page offsets, and O^T leaves every lane
 // with D / 4 neighbouring elements of its query row.
 template <typename T, int D, int kTiles>
-__global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void asd_attend_kernel(AttentionArgs a, float* partials) {
+__global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_attend_kernel(AttentionArgs a, float* partials,
+                                                                       Cut* cuts) {
     constexpr int kRows = 16 * kTiles, NC = D / 16, kSteps = D / 32, kVecs = (NC + 7) / 8;
     constexpr bool kQueriesInLds = kTiles > 2;
     typedef typename Half<T>::x8 x8;
@@ -167,61 +209,65 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void asd_attend_k
     __shared__ int64_t offsets[kAttendWaves][kStrip];
     __shared__ float joined[kAttendWaves][16][D + 4];
     __shared__ float tops[kAttendWaves][16], sums[kAttendWaves][16];
+    __shared__ int32_t row_p[kRows];                  // the block's row of every row of the tile
     __shared__ x8 queries[kQueriesInLds ? kTiles * kSteps * 64 : 1];
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
     const asd_paged_cache& cache = a.b.cache;
     const int32_t group = a.num_q_heads / cache.num_heads;
-    // neighbouring stretches, which may share keys and values, on one XCD
-    const int64_t wgs = gridDim.x, eighth = wgs / 8;
-    const int64_t id = blockIdx.x < eighth * 8 ? (blockIdx.x % 8) * eighth + blockIdx.x / 8 : blockIdx.x;
-    Where at = locate(a.b, group, kRows, id, wgs, blockIdx.x == 0, box, &where_box);
-    int64_t left = bound_of(at.total, wgs, id + 1) - bound_of(at.total, wgs, id);
-    const float per = a.scale * 1.44269504f;
+    Where at = locate<kRows>(a.b, group, box, &where_box);
+    if (at.id < 0) {
+        if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{0, 0, 0, 0, 0, 0};
+        return;
+    }
+    int64_t left = min(at.per, at.total - at.id * at.per);
+    const float per = __uint_as_float((uint32_t)uniform((int32_t)__float_as_uint(a.scale * 1.44269504f)));
 
     while (left > 0) {
-        const int32_t count = max(a.b.block_lens[at.request], 0) + 1;
-        const int64_t cached64 = a.b.cache_lens[at.request];
-        const int64_t pairs = (int64_t)count * group, units = (cached64 + count + kUnit - 1) / kUnit;
-        const int64_t tiles = (pairs + kRows - 1) / kRows;
+        const int32_t count = at.count;
+        const int64_t cached64 = at.cached;
         uint32_t unused = 0;
-        if (units_of(a.b, group, kRows, at.row, count, cached64, unused) <= at.unit) {
+        if (units_of<kRows>(a.b, group, at.row, count, cached64, unused) <= at.unit) {
             // on to the next request
-            at.row = a.b.row_offsets ? a.b.row_offsets[at.request + 1] : at.row + count;
+            at.row = a.b.row_offsets ? uniform(a.b.row_offsets[at.request + 1]) : at.row + count;
             at.request += 1;
+            at.count = uniform(rows_of_block(a.b.block_lens[at.request]));
+            at.cached = uniform(a.b.cache_lens[at.request]);
             at.unit = 0;
             continue;
         }
-        const int64_t item = at.unit / units, from = at.unit - item * units;
+        const int32_t pairs = count * group, tiles = (pairs + kRows - 1) / kRows;
+        const int64_t units = (cached64 + count + kUnit - 1) / kUnit;
+        const int64_t item = quotient(at.unit, units), from = at.unit - item * units;
         const int64_t to = from + left < units ? from + left : units;
-        const int32_t head = (int32_t)(item / tiles);
-        const int64_t first = (item - head * tiles) * kRows;      // of the pairs
+        const int32_t head = (int32_t)quotient(item, tiles);
+        const int32_t first = (int32_t)(item - (int64_t)head * tiles) * kRows;      // of the pairs
         at.unit += to - from;
         left -= to - from;
 
+        const int tid = fresh(threadIdx.x), lane = tid & 63, wave = uniform(tid >> 6), n = lane & 15, g = lane >> 4;
         // the tile's queries: B operands, lane n's row, 8 elements of every 32
         const auto query = [&](int tile, int step) -> x8 {
-            const int64_t m = first + 16 * tile + n;
+            const int32_t m = first + 16 * tile + n;
             if (m >= pairs) return x8{};
-            const int64_t p = m / group;
-            const int32_t x = (int32_t)(m - p * group);
+            const int32_t p = m / group;
             return *(const x8*)((const T*)a.q + (at.row + p) * a.q_stride +
-                                ((int64_t)head * group + x) * D + 32 * step + 8 * g);
+                                (head * group + m - p * group) * D + 32 * step + 8 * g);
         };
         x8 q[kQueriesInLds ? 1 : kTiles][kSteps];
+        __syncthreads();
+        if (tid < kRows) row_p[tid] = min(first + tid, pairs - 1) / group;
         if constexpr (kQueriesInLds) {
-            __syncthreads();
             for (int tile = wave; tile < kTiles; tile += kAttendWaves)
                 #pragma unroll
                 for (int step = 0; step < kSteps; ++step)
                     queries[(tile * kSteps + step) * 64 + lane] = query(tile, step);
-            __syncthreads();
         } else {
-            #pragma unroll
+#pragma unroll
             for (int tile = 0; tile < kTiles; ++tile)
-                #pragma unroll
+#pragma unroll
                 for (int step = 0; step < kSteps; ++step) q[tile][step] = query(tile, step);
         }
+        __syncthreads();
 
         f32x4 o[kTiles][NC];
         float ref[kTiles], sum[kTiles];
@@ -234,165 +280,93 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void asd_attend_k
         }
         // a chain's rows see no token behind the tile's last one
         const int32_t cached = (int32_t)cached64, end_all = cached + count;
-        const int32_t last_p = (int32_t)((min(first + kRows, pairs) - 1) / group);
+        const int32_t last_p = uniform(row_p[kRows - 1]);
         const int32_t end = a.mask ? end_all : cached + last_p + 1;
         const int32_t strip_end = (int32_t)min(to * kUnit, (int64_t)end);
         int32_t strip = (int32_t)(from * kUnit) + wave * kStrip;
         int64_t* const offs = offsets[wave];
         const int32_t* const table = cache.page_table + (int64_t)at.request * cache.max_pages;
-        const T* const keys = (const T*)cache.keys + (int64_t)head * cache.head_stride;
-        const T* const values = (const T*)cache.values + (int64_t)head * cache.head_stride;
+        // at the lane's part of a token: 8 elements of every 32 of its key, D / 16 of its value
+        const char* const keys = (const char*)((const T*)cache.keys + (int64_t)head * cache.head_stride + 8 * g);
+        const char* const values = (const char*)((const T*)cache.values + (int64_t)head * cache.head_stride + NC * n);
 
-        // A strip's page ids (lanes l and l + 32 hold token l), its tokens' offsets (negative: not
-        // there), and its keys and values as operands.
-        const auto page_of = [&](int32_t t0) -> int32_t {
+        // A strip's page ids (lanes l and l + 32 hold token l; tokens behind the last one take
+        // its page) and, from them, its tokens' byte offsets in LDS; the mask of the tokens that
+        // are there, the others' offsets being 0.
+        const auto page_at = [&](int32_t t) { return (int32_t)(__umulhi(2 * (uint32_t)t, a.page_magic) >> a.page_shift); };
+        const auto page_of = [&](int32_t t0) -> int32_t { return table[page_at(min(t0 + (lane & 31), end_all - 1))]; };
+        const auto put_offsets = [&](int32_t t0, int32_t page) -> uint32_t {
             const int32_t t = t0 + (lane & 31);
-            return t < end_all ? table[(uint32_t)t / (uint32_t)cache.page_size] : 0;
+            const bool ok = t < end_all && (uint32_t)page < (uint32_t)cache.num_pages;
+            const int32_t slot = t - page_at(t) * cache.page_size;
+            const int64_t off = ((int64_t)page * cache.page_stride + (int64_t)slot * cache.token_stride) * 2;
+            wave_sync();
+            if (lane < 32) offs[lane] = ok ? off : 0;
+            wave_sync();
+            return (uint32_t)__ballot(ok);
         };
         x8 k[2][kSteps];
         u32x4 v[8][kVecs];
-        const auto put_offsets = [&](int32_t t0, int32_t page) -> bool {
-            const int32_t t = t0 + (lane & 31);
-            const bool in = t < end_all, ok = in && page >= 0 && page < cache.num_pages;
-            if (in && !ok) atomicOr(a.b.error_word, kDecodeErrCache);
-            const int32_t slot = (int32_t)((uint32_t)t % (uint32_t)cache.page_size);
-            wave_sync();
-            if (lane < 32)
-                offs[lane] = ok ? (int64_t)page * cache.page_stride + (int64_t)slot * cache.token_stride : -1;
-            wave_sync();
-            return __all(ok);
-        };
         const auto load_keys = [&]() {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const T* src = keys + max(offs[16 * h + n], (int64_t)0) + 8 * g;
+                const char* src = keys + offs[16 * h + n];
 #pragma unroll
-                for (int step = 0; step < kSteps; ++step) k[h][step] = *(const x8*)(src + 32 * step);
+                for (int step = 0; step < kSteps; ++step) k[h][step] = *(const x8*)(src + 64 * step);
             }
         };
         const auto load_values = [&]() {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const T* src = values + max(offs[(j & 3) + 4 * g + 16 * (j >> 2)], (int64_t)0) + NC * n;
+                const char* src = values + offs[(j & 3) + 4 * g + 16 * (j >> 2)];
                 if constexpr (NC == 4) {
                     const u32x2 w = *(const u32x2*)src;
                     v[j][0].x = w.x;
                     v[j][0].y = w.y;
                 } else {
 #pragma unroll
-                    for (int x = 0; x < kVecs; ++x) v[j][x] = *(const u32x4*)(src + 8 * x);
+                    for (int x = 0; x < kVecs; ++x) v[j][x] = *(const u32x4*)(src + 16 * x);
                 }
             }
         };
-
-        int32_t page = 0;
-        bool whole = false;
-        if (strip < strip_end) {
-            page = page_of(strip);
-            whole = put_offsets(strip, page);
-            load_keys();
-            load_values();
-            page = page_of(strip + kUnit);
-        }
-        for (; strip < strip_end; strip += kUnit) {
-            const bool more = strip + kUnit < strip_end;
-            // Which of the lane's 8 tokens its rows see, 8 bits a tile, and which are there at all.
-            const bool plain = whole && strip + kStrip <= cached;
-            uint32_t seen = ~0u, there = 0xffu;
-            if (!plain) {
-                seen = there = 0;
-#pragma unroll 1
-                for (int j = 0; j < 8; ++j) {
-                    const int32_t at_strip = (j & 3) + 4 * g + 16 * (j >> 2), x = strip + at_strip - cached;
-                    if (offs[at_strip] < 0) continue;
-                    there |= 1u << j;
-#pragma unroll 1
-                    for (int tile = 0; tile < kTiles; ++tile) {
-                        const int64_t p = min(first + 16 * tile + n, pairs - 1) / group;
-                        const bool sees = x < 0 || (!a.mask ? x <= p
-                                                            : x < 64 * (int64_t)a.mask_words &&
-                            ((a.mask[(at.row + p) * a.mask_words + x / 64] >> (x % 64)) & 1) != 0);
-                        seen |= (uint32_t)sees << (8 * tile + j);
-                    }
-                }
+        // Scores and weights of tile `tile`, whose lane sees the tokens of `seen` (8 bits).
+        x8 w[kTiles];
+        const auto weigh = [&](int tile, bool all, uint32_t seen) {
+            f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
+#pragma unroll
+            for (int step = 0; step < kSteps; ++step) {
+                x8 qq;
+                if constexpr (kQueriesInLds) qq = queries[(tile * kSteps + step) * 64 + lane];
+                else qq = q[tile][step];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) s[h] = Half<T>::mfma(k[h][step], qq, s[h]);
             }
-
-            x8 w[kTiles];
+            float x[8];
 #pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile) {
-                f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
-#pragma unroll
-                for (int step = 0; step < kSteps; ++step) {
-                    x8 qq;
-                    if constexpr (kQueriesInLds) qq = queries[(tile * kSteps + step) * 64 + lane];
-                    else qq = q[tile][step];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) s[h] = Half<T>::mfma(k[h][step], qq, s[h]);
-                }
-                float x[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = s[j >> 2][j & 3] * per;
-                if (!plain) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = (seen >> (8 * tile + j)) & 1 ? x[j] : -INFINITY;
-                }
-                float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                                  fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-                top = rows_max(top);
-                if (__any(top > ref[tile] + kLead)) {
-                    const float now = top > ref[tile] + kLead ? top - kSet : ref[tile];
-                    const float keep = now == ref[tile] ? 1.0f : __builtin_amdgcn_exp2f(ref[tile] - now);
-                    ref[tile] = now;
-                    sum[tile] *= keep;
-#pragma unroll
-                    for (int c = 0; c < NC; ++c) o[tile][c] *= keep;
-                }
-                const float from_ref = ref[tile] == -INFINITY ? 0.0f : ref[tile];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    x[j] = __builtin_amdgcn_exp2f(x[j] - from_ref);
-                    sum[tile] += x[j];
-                    w[tile][j] = (T)x[j];
-                }
+            for (int j = 0; j < 8; ++j) {
+                x[j] = s[j >> 2][j & 3] * per;
+                if (!all) x[j] = (seen >> j) & 1 ? x[j] : -INFINITY;
             }
-            bool next_whole = false;
-            if (more) {
-                next_whole = put_offsets(strip + kUnit, page);
-                load_keys();
-                page = page_of(strip + 2 * kUnit);
+            float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
+                              fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            top = rows_max(top);
+            if (__any(top > ref[tile] + kLead)) {
+                const float now = top > ref[tile] + kLead ? top - kSet : ref[tile];
+                const float keep = now == ref[tile] ? 1.0f : __builtin_amdgcn_exp2f(ref[tile] - now);
+                ref[tile] = now;
+                sum[tile] *= keep;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) o[tile][c] *= keep;
             }
-
-            // Values that are not there are zeros.  A token that holds an infinity or a NaN
-            // would reach every row through its weight 0: it leaves the product and is added by
-            // hand to the rows that see it.
-            uint32_t odd = 0;
-            if (!plain) {
+            const float from_ref = ref[tile] == -INFINITY ? 0.0f : ref[tile];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    bool special = false;
-#pragma unroll
-                    for (int x = 0; x < kVecs; ++x)
-#pragma unroll
-                        for (int y = 0; y < (NC == 4 ? 2 : 4); ++y) {
-                            const uint32_t word = (there >> j) & 1 ? v[j][x][y] : 0u;
-                            v[j][x][y] = word;
-                            constexpr uint32_t e = Half<T>::kExponent;
-                            special |= (word & e) == e || (word >> 16 & e) == e;
-                        }
-                    const uint64_t lanes = __ballot(special);
-#pragma unroll
-                    for (int gg = 0; gg < 4; ++gg)
-                        odd |= (uint32_t)((lanes >> (16 * gg) & 0xffff) != 0) << ((j & 3) + 4 * gg + 16 * (j >> 2));
-                }
-                if (odd != 0) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const bool mine = (odd >> ((j & 3) + 4 * g + 16 * (j >> 2))) & 1;
-#pragma unroll
-                        for (int x = 0; x < kVecs; ++x) v[j][x] = mine ? u32x4{0, 0, 0, 0} : v[j][x];
-                    }
-                }
+            for (int j = 0; j < 8; ++j) {
+                x[j] = __builtin_amdgcn_exp2f(x[j] - from_ref);
+                sum[tile] += x[j];
+                w[tile][j] = (T)x[j];
             }
+        };
+        const auto add_values = [&]() {
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
                 u32x4 f;
@@ -404,6 +378,96 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void asd_attend_k
                 for (int tile = 0; tile < kTiles; ++tile)
                     o[tile][c] = Half<T>::mfma(__builtin_bit_cast(x8, f), w[tile], o[tile][c]);
             }
+        };
+
+        // Strips that every row sees whole.  The next strip's keys are loaded once this one's are
+        // used, its values likewise, and the page ids of the one after it a strip ahead, so that
+        // no load is waited for where it is issued.
+        uint32_t valid = 0;
+        if (strip < strip_end) {
+            valid = put_offsets(strip, page_of(strip));
+            if (valid == ~0u && strip + kStrip <= cached) {
+                int32_t page = page_of(strip + kUnit);
+                __builtin_amdgcn_sched_barrier(0);      // the order of the loop, so that its waits are short
+                load_keys();
+                __builtin_amdgcn_sched_barrier(0);
+                load_values();
+                // (the loads stay here: sunk into the loop they would not run ahead)
+                asm volatile("" ::: "memory");
+                do {
+                    valid = put_offsets(strip + kUnit, page);
+#pragma unroll
+                    for (int tile = 0; tile < kTiles; ++tile) {
+                        weigh(tile, true, 0);
+                        if (kTiles > 2) __builtin_amdgcn_sched_barrier(0);
+                    }
+                    page = page_of(strip + 2 * kUnit);
+                    load_keys();
+                    __builtin_amdgcn_sched_barrier(0);
+                    add_values();
+                    __builtin_amdgcn_sched_barrier(0);
+                    load_values();
+                    asm volatile("" ::: "memory");
+                    strip += kUnit;
+                } while (strip < strip_end && valid == ~0u && strip + kStrip <= cached);
+            }
+        }
+        // The others: the block's own tokens, the strip that the sequence ends in, bad pages.
+#pragma unroll 1
+        while (strip < strip_end) {
+            if (lane < 32 && strip + lane < end_all && !((valid >> lane) & 1))
+                atomicOr(a.b.error_word, kDecodeErrCache);
+            load_keys();
+            load_values();
+            // which of the lane's 8 tokens its rows see, 8 bits a tile, and which are there at all
+            uint32_t seen = 0, there = 0;
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+                const int32_t at_strip = (j & 3) + 4 * g + 16 * (j >> 2), x = strip + at_strip - cached;
+                if (!((valid >> at_strip) & 1)) continue;
+                there |= 1u << j;
+#pragma unroll 1
+                for (int tile = 0; tile < kTiles; ++tile) {
+                    const int32_t p = row_p[16 * tile + n];
+                    const bool sees = x < 0 || (!a.mask ? x <= p
+                                                        : x < 64 * (int64_t)a.mask_words &&
+                        ((a.mask[(at.row + p) * a.mask_words + x / 64] >> (x % 64)) & 1) != 0);
+                    seen |= (uint32_t)sees << (8 * tile + j);
+                }
+            }
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile) weigh(tile, false, seen >> (8 * tile));
+
+            // Values that are not there are zeros.  A token that holds an infinity or a NaN
+            // would reach every row through its weight 0: it leaves the product and is added by
+            // hand to the rows that see it.
+            uint32_t odd = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                bool special = false;
+#pragma unroll
+                for (int x = 0; x < kVecs; ++x)
+#pragma unroll
+                    for (int y = 0; y < (NC == 4 ? 2 : 4); ++y) {
+                        const uint32_t word = (there >> j) & 1 ? v[j][x][y] : 0u;
+                        v[j][x][y] = word;
+                        constexpr uint32_t e = Half<T>::kExponent;
+                        special |= (word & e) == e || (word >> 16 & e) == e;
+                    }
+                const uint64_t lanes = __ballot(special);
+#pragma unroll
+                for (int gg = 0; gg < 4; ++gg)
+                    odd |= (uint32_t)((lanes >> (16 * gg) & 0xffff) != 0) << ((j & 3) + 4 * gg + 16 * (j >> 2));
+            }
+            if (odd != 0) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const bool mine = (odd >> ((j & 3) + 4 * g + 16 * (j >> 2))) & 1;
+#pragma unroll
+                    for (int x = 0; x < kVecs; ++x) v[j][x] = mine ? u32x4{0, 0, 0, 0} : v[j][x];
+                }
+            }
+            add_values();
             if (odd != 0) {
 #pragma unroll
                 for (int tile = 0; tile < kTiles; ++tile) {
@@ -415,13 +479,10 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void asd_attend_k
                     wave_sync();
 #pragma unroll 1
                     for (uint32_t rest = odd; rest != 0; rest &= rest - 1) {
-                        const int32_t at_strip = __builtin_ctz(rest), t = strip + at_strip;
+                        const int32_t at_strip = __builtin_ctz(rest);
                         const float weight = joined[wave][n][at_strip];
                         if (weight == -1.0f) continue;
-                        const int64_t off =
-                            (int64_t)table[(uint32_t)t / (uint32_t)cache.page_size] * cache.page_stride +
-                            (int64_t)((uint32_t)t % (uint32_t)cache.page_size) * cache.token_stride;
-                        const T* src = values + off + 4 * NC * g;
+                        const T* src = (const T*)(values - 2 * NC * n + offs[at_strip]) + 4 * NC * g;
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -430,36 +491,36 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void asd_attend_k
                     }
                 }
             }
-            if (more) load_values();
-            whole = next_whole;
+            strip += kUnit;
+            if (strip < strip_end) valid = put_offsets(strip, page_of(strip));
         }
 
         // the wavefronts' sums, joined tile by tile
+        const int tid_end = fresh(tid), n_end = tid_end & 15, g_end = tid_end >> 4 & 3, row = tid_end >> 4;
         const bool complete = from == 0 && to == units;
-        float* const slot = partials + (2 * id + (from > 0 ? 0 : 1)) * (int64_t)(kRows * (D + 2));
+        float* const slot = partials + (2 * at.id + (from > 0 ? 0 : 1)) * (int64_t)(kRows * (D + 2));
         #pragma unroll
         for (int tile = 0; tile < kTiles; ++tile) {
             sum[tile] = rows_sum(sum[tile]);
             if (ref[tile] == -INFINITY && sum[tile] != sum[tile]) ref[tile] = 0.0f;   // every score a NaN
             __syncthreads();
-            if (g == 0) {
-                tops[wave][n] = ref[tile];
-                sums[wave][n] = sum[tile];
+            if (g_end == 0) {
+                tops[wave][n_end] = ref[tile];
+                sums[wave][n_end] = sum[tile];
             }
             __syncthreads();
-            float best = tops[0][n];
+            float best = tops[0][n_end];
             #pragma unroll
-            for (int w = 1; w < kAttendWaves; ++w) best = fmaxf(best, tops[w][n]);
+            for (int w = 1; w < kAttendWaves; ++w) best = fmaxf(best, tops[w][n_end]);
             const float mine = ref[tile] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[tile] - best);
             #pragma unroll
             for (int r = 0; r < 4; ++r)
                 #pragma unroll
                 for (int c = 0; c < NC; c += 4)
-                    *(f32x4*)&joined[wave][n][4 * NC * g + NC * r + c] =
+                    *(f32x4*)&joined[wave][n_end][4 * NC * g_end + NC * r + c] =
                         f32x4{o[tile][c][r], o[tile][c + 1][r], o[tile][c + 2][r], o[tile][c + 3][r]} * mine;
             __syncthreads();
             // 16 threads a row, each every 16th vector of 4 elements
-            const int row = threadIdx.x >> 4;
             best = tops[0][row];
             #pragma unroll
             for (int w = 1; w < kAttendWaves; ++w) best = fmaxf(best, tops[w][row]);
@@ -468,22 +529,21 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void asd_attend_k
             for (int w = 0; w < kAttendWaves; ++w)
                 total += tops[w][row] == -INFINITY ? 0.0f
                                                    : sums[w][row] * __builtin_amdgcn_exp2f(tops[w][row] - best);
-            const int64_t m = first + 16 * tile + row;
-            if (!complete && (threadIdx.x & 15) == 0) {
+            const int32_t m = first + 16 * tile + row;
+            if (!complete && n_end == 0) {
                 slot[kRows * D + 16 * tile + row] = best;
                 slot[kRows * (D + 1) + 16 * tile + row] = total;
             }
-            const int64_t p = m / group;
+            const int32_t p = row_p[16 * tile + row];
             const float over = best == -INFINITY ? 0.0f : 1.0f / total;
-            for (int e = 4 * (threadIdx.x & 15); e < D; e += 64) {
+            for (int e = 4 * n_end; e < D; e += 64) {
                 f32x4 x = *(const f32x4*)&joined[0][row][e];
                 #pragma unroll
                 for (int w = 1; w < kAttendWaves; ++w) x += *(const f32x4*)&joined[w][row][e];
                 if (!complete) {
                     *(f32x4*)&slot[(16 * tile + row) * D + e] = x;
                 } else if (m < pairs) {
-                    T* dst = (T*)a.out + ((at.row + p) * a.num_q_heads + (int64_t)head * group +
-                                          (m - p * group)) * D + e;
+                    T* dst = (T*)a.out + ((at.row + p) * a.num_q_heads + head * group + m - p * group) * D + e;
                     typename Half<T>::x2 y[2];
                     #pragma unroll
                     for (int z = 0; z < 4; ++z) y[z / 2][z % 2] = (T)(x[z] * over);
@@ -492,68 +552,108 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void asd_attend_k
             }
         }
         __syncthreads();
+        if (tid_end == 0 && left == 0)
+            cuts[blockIdx.x] = Cut{at.row, (int32_t)at.id, head, first, pairs,
+                              from == 0 && !complete ? 1 + (int32_t)quotient(units - to + at.per - 1, at.per) : 0};
     }
 }
 
-// Joins the partials of the item that the bound of two stretches, blockIdx.x and the one before, cuts; the
-// first of an item's bounds does it.  A wavefront takes a row.
+// Joins the partials of the item that is cut by the end of workgroup blockIdx.x's stretch, if one is; a
+// workgroup takes four of its rows: a wavefront each where the parts are few, else one
+// after the other with the parts shared out over groups of D / 4 lanes.
+constexpr int kFewParts = 8;
 template <typename T, int D, int kTiles>
 __global__ __launch_bounds__(kAttendThreads) void asd_attend_join_kernel(AttentionArgs a, const float* partials,
-                                                                         int64_t wgs) {
-    constexpr int kRows = 16 * kTiles, kPer = D / 64;
-    __shared__ int64_t box[kAttendWaves];
-    __shared__ Where where_box;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int32_t group = a.num_q_heads / a.b.cache.num_heads;
-    const int64_t id = blockIdx.x + 1;
-    const Where at = locate(a.b, group, kRows, id, wgs, false, box, &where_box);
-    if (at.request < 0) return;
-    const auto bound = [&](int64_t x) { return bound_of(at.total, wgs, x); };
-    const int32_t count = max(a.b.block_lens[at.request], 0) + 1;
-    const int64_t pairs = (int64_t)count * group;
-    const int64_t units = (a.b.cache_lens[at.request] + count + kUnit - 1) / kUnit;
-    const int64_t tiles = (pairs + kRows - 1) / kRows;
-    const int64_t item = at.unit / units, inside = at.unit - item * units;
-    const int64_t u = bound(id), begin = u - inside, end = begin + units;
-    if (inside == 0 || bound(id - 1) > begin) return;
-    const int32_t head = (int32_t)(item / tiles);
-    const int64_t first = (item - head * tiles) * kRows;
-    int64_t last = id;                                   // the last stretch of the item
-    while (bound(last + 1) < end) ++last;
+                                                                         const Cut* cuts) {
+    constexpr int kRows = 16 * kTiles, kPer = D / 64, kCols = D / 4, kGroups = kAttendThreads / kCols;
     constexpr int64_t kSize = (int64_t)kRows * (D + 2);
-    const int64_t parts = last - id + 2;
-    const auto part = [&](int64_t j) { return partials + (2 * (id - 1 + j) + (j == 0 ? 1 : 0)) * kSize; };
-    for (int row = (int)blockIdx.y * kAttendWaves + wave; row < kRows; row += kAttendWaves * (int)gridDim.y) {
-        const int64_t m = first + row;
-        if (m >= pairs) break;
-        float best = -INFINITY;
-        for (int64_t j = lane; j < parts; j += 64)
-            if (bound(id - 1 + j) < bound(id + j)) best = fmaxf(best, part(j)[kRows * D + row]);
-        for (int s = 32; s > 0; s >>= 1) best = fmaxf(best, __shfl_xor(best, s));
-        float total = 0.0f, o[kPer];
+    __shared__ float factor[kAttendThreads];
+    __shared__ f32x4 sums[kGroups][kCols];
+    __shared__ float box[2][kAttendWaves];
+    const int lane = threadIdx.x & 63, wave = uniform((int32_t)threadIdx.x >> 6);
+    const Cut cut = cuts[blockIdx.x];
+    if (cut.parts == 0) return;
+    const int64_t id = cut.id;
+    const int32_t group = a.num_q_heads / a.b.cache.num_heads;
+    const auto part = [&](int j) { return partials + (2 * (id + j) + (j == 0 ? 1 : 0)) * kSize; };
+    const auto row_of = [&](int32_t m) {
+        const int32_t p = m / group;
+        return (T*)a.out + ((cut.row + p) * a.num_q_heads + cut.head * group + m - p * group) * D;
+    };
+    if (cut.parts <= kFewParts) {
+        const int row = (int)blockIdx.y * kAttendWaves + wave;
+        const int32_t m = cut.first + row;
+        if (m >= cut.pairs) return;
+        float top[kFewParts], o[kPer];
+        float best = -INFINITY, total = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kFewParts; ++j) {
+            top[j] = j < cut.parts ? part(j)[kRows * D + row] : -INFINITY;
+            best = fmaxf(best, top[j]);
+        }
+#pragma unroll
         for (int e = 0; e < kPer; ++e) o[e] = 0.0f;
-        for (int64_t j0 = 0; j0 < parts; j0 += 64) {
+#pragma unroll
+        for (int j = 0; j < kFewParts; ++j) {
+            if (j >= cut.parts) break;
+            const float f = top[j] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[j] - best);
+            const float* x = part(j);
+            total = fmaf(f, x[kRows * (D + 1) + row], total);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) o[e] = fmaf(f, x[row * D + kPer * lane + e], o[e]);
+        }
+        const float over = best == -INFINITY ? 0.0f : 1.0f / total;
+        T* dst = row_of(m);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) dst[kPer * lane + e] = (T)(o[e] * over);
+        return;
+    }
+    const int col = threadIdx.x % kCols, mine = threadIdx.x / kCols;
+    for (int r = 0; r < kAttendWaves; ++r) {
+        const int row = (int)blockIdx.y * kAttendWaves + r;
+        const int32_t m = cut.first + row;
+        if (m >= cut.pairs) return;
+        float best = -INFINITY;
+        for (int j = threadIdx.x; j < cut.parts; j += kAttendThreads)
+            best = fmaxf(best, part(j)[kRows * D + row]);
+        for (int s = 32; s > 0; s >>= 1) best = fmaxf(best, __shfl_xor(best, s));
+        __syncthreads();
+        if (lane == 0) box[0][wave] = best;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kAttendWaves; ++w) best = fmaxf(best, box[0][w]);
+        float total = 0.0f;
+        f32x4 o = {0, 0, 0, 0};
+        for (int j0 = 0; j0 < cut.parts; j0 += kAttendThreads) {
+            const int j = j0 + threadIdx.x, here = min(kAttendThreads, cut.parts - j0);
             float f = 0.0f;
-            if (j0 + lane < parts && bound(id - 1 + j0 + lane) < bound(id + j0 + lane)) {
-                const float* x = part(j0 + lane);
-                const float top = x[kRows * D + row];
+            if (j < cut.parts) {
+                const float top = part(j)[kRows * D + row];
                 f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - best);
-                total += top == -INFINITY ? 0.0f : f * x[kRows * (D + 1) + row];
+                total = fmaf(f, part(j)[kRows * (D + 1) + row], total);
             }
-            const int here = (int)min((int64_t)64, parts - j0);
-
-            for (int j = 0; j < here; ++j) {
-                const float fj = __shfl(f, j);
-                const float* x = part(j0 + j) + row * D;
-                if (fj != 0.0f)
-                    for (int e = 0; e < kPer; ++e) o[e] = fmaf(fj, x[kPer * lane + e], o[e]);
+            __syncthreads();
+            factor[threadIdx.x] = f;
+            __syncthreads();
+#pragma unroll 4
+            for (int x = mine; x < here; x += kGroups) {
+                const f32x4 y = *(const f32x4*)&part(j0 + x)[row * D + 4 * col];
+                o += y * factor[x];
             }
         }
         for (int s = 32; s > 0; s >>= 1) total += __shfl_xor(total, s);
-        const float over = best == -INFINITY ? 0.0f : 1.0f / total;
-        const int64_t p = m / group;
-        T* dst = (T*)a.out + ((at.row + p) * a.num_q_heads + (int64_t)head * group + (m - p * group)) * D;
-        for (int e = 0; e < kPer; ++e) dst[kPer * lane + e] = (T)(o[e] * over);
+        if (lane == 0) box[1][wave] = total;
+        sums[mine][col] = o;
+        __syncthreads();
+        if (mine == 0) {
+            total = box[1][0] + box[1][1] + box[1][2] + box[1][3];
+#pragma unroll
+            for (int x = 1; x < kGroups; ++x) o += sums[x][col];
+            const float over = best == -INFINITY ? 0.0f : 1.0f / total;
+            T* dst = row_of(m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dst[4 * col + e] = (T)(o[e] * over);
+        }
     }
 }
 
@@ -561,40 +661,48 @@ __global__ __launch_bounds__(kAttendThreads) void asd_attend_join_kernel(Attenti
 
 namespace {
 
-// 16-row tiles of an item: what the batch's blocks fill on average.  Wide heads take at most two.
+// 16-row tiles of an item: the (row, head) pairs of an average block spread evenly over the fewest
+// items, of as many tiles as the registers hold.
 int tiles_of(int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t num_requests,
              int64_t total_rows) {
-    const int64_t pairs = total_rows / num_requests * (num_q_heads / num_kv_heads);
-    return pairs <= 16 ? 1 : pairs <= 32 || head_dim == 256 ? 2 : 4;
+    const int64_t most = head_dim == 64 ? 4 : head_dim == 128 ? 3 : 2;
+    const int64_t pairs = (total_rows + num_requests - 1) / num_requests * (num_q_heads / num_kv_heads);
+    const int64_t tiles = (pairs + 15) / 16, items = (tiles + most - 1) / most;
+    return (int)((tiles + items - 1) / items);
 }
 
-// Two workgroups fit on a compute unit.
-int64_t stretches_of(int cus) { return 2 * (int64_t)cus; }
+size_t partial_bytes(int64_t wgs, int head_dim, int tiles) {
+    return (size_t)(2 * wgs) * 16 * tiles * (head_dim + 2) * sizeof(float);
+}
 
 template <typename T, int D, int kTiles>
-hipError_t attend(const AttentionArgs& a, float* partials, int64_t wgs, hipStream_t stream) {
-    asd_attend_kernel<T, D, kTiles><<<(unsigned)wgs, kAttendThreads, 0, stream>>>(a, partials);
-    hipError_t err = hipGetLastError();
-    if (err != hipSuccess || wgs < 2) return err;
+hipError_t attend(const AttentionArgs& a, void* workspace, int64_t wgs, hipStream_t stream) {
+    float* const partials = (float*)workspace;
+    Cut* const cuts = (Cut*)((char*)workspace + partial_bytes(wgs, D, kTiles));
+    asd_attend_kernel<T, D, kTiles><<<(unsigned)wgs, kAttendThreads, 0, stream>>>(a, partials, cuts);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
     asd_attend_join_kernel<T, D, kTiles>
-        <<<dim3((unsigned)(wgs - 1), kTiles), kAttendThreads, 0, stream>>>(a, partials, wgs);
+        <<<dim3((unsigned)wgs, 4 * kTiles), kAttendThreads, 0, stream>>>(a, partials, cuts);
     return hipGetLastError();
 }
 
 template <typename T>
-hipError_t attend_any(const AttentionArgs& a, float* partials, int64_t wgs, int tiles, hipStream_t stream) {
-    switch (a.b.cache.head_dim) {
-        case 64:
-            return tiles == 1 ? attend<T, 64, 1>(a, partials, wgs, stream)
-                   : tiles == 2 ? attend<T, 64, 2>(a, partials, wgs, stream)
-                                : attend<T, 64, 4>(a, partials, wgs, stream);
-        case 128:
-            return tiles == 1 ? attend<T, 128, 1>(a, partials, wgs, stream)
-                   : tiles == 2 ? attend<T, 128, 2>(a, partials, wgs, stream)
-                                : attend<T, 128, 4>(a, partials, wgs, stream);
-        default:
-            return tiles == 1 ? attend<T, 256, 1>(a, partials, wgs, stream)
-                              : attend<T, 256, 2>(a, partials, wgs, stream);
+hipError_t attend_any(const AttentionArgs& a, void* workspace, int64_t wgs, int tiles, hipStream_t stream) {
+    const int d = a.b.cache.head_dim;
+    switch (tiles) {
+        case 1:
+            return d == 64    ? attend<T, 64, 1>(a, workspace, wgs, stream)
+                   : d == 128 ? attend<T, 128, 1>(a, workspace, wgs, stream)
+                              : attend<T, 256, 1>(a, workspace, wgs, stream);
+        case 2:
+            return d == 64    ? attend<T, 64, 2>(a, workspace, wgs, stream)
+                   : d == 128 ? attend<T, 128, 2>(a, workspace, wgs, stream)
+                              : attend<T, 256, 2>(a, workspace, wgs, stream);
+        case 3:
+            return d == 64 ? attend<T, 64, 3>(a, workspace, wgs, stream)
+                           : attend<T, 128, 3>(a, workspace, wgs, stream);
+        default: return attend<T, 64, 4>(a, workspace, wgs, stream);
     }
 }
 
@@ -604,21 +712,21 @@ size_t attention_workspace_bytes(int32_t num_q_heads, int32_t num_kv_heads, int3
                                  int32_t num_requests, int64_t total_rows, int cus) {
     if (num_requests == 0) return 0;
     const int tiles = tiles_of(num_q_heads, num_kv_heads, head_dim, num_requests, total_rows);
-    return (size_t)(2 * stretches_of(cus)) * 16 * tiles * (head_dim + 2) * sizeof(float);
+    const int64_t wgs = (int64_t)cus * resident(head_dim, tiles);
+    return partial_bytes(wgs, head_dim, tiles) + (size_t)wgs * sizeof(Cut);
 }
 
 hipError_t launch_block_attention(const AttentionArgs& a, bool bf16, void* workspace, int cus,
                                   hipStream_t stream) {
     const asd_paged_cache& c = a.b.cache;
+    AttentionArgs b = a;
+    b.page_shift = 0;
+    while (((int64_t)1 << b.page_shift) < c.page_size) ++b.page_shift;
+    b.page_magic = (uint32_t)((((uint64_t)1 << (31 + b.page_shift)) + c.page_size - 1) / c.page_size);
     const int tiles = tiles_of(a.num_q_heads, c.num_heads, c.head_dim, a.b.num_requests, a.b.total_rows);
-    // no more stretches than units the batch can have
-    const int64_t group = a.num_q_heads / c.num_heads;
-    const __int128 items = (__int128)c.num_heads * (a.b.num_requests + a.b.total_rows * group / (16 * tiles));
-    const __int128 units = items * (((int64_t)c.max_pages * c.page_size + kUnit - 1) / kUnit);
-    int64_t wgs = stretches_of(cus);
-    if (units < wgs) wgs = (int64_t)units;
-    return bf16 ? attend_any<__bf16>(a, (float*)workspace, wgs, tiles, stream)
-                : attend_any<_Float16>(a, (float*)workspace, wgs, tiles, stream);
+    const int64_t wgs = (int64_t)cus * resident(c.head_dim, tiles);
+    return bf16 ? attend_any<__bf16>(b, workspace, wgs, tiles, stream)
+                : attend_any<_Float16>(b, workspace, wgs, tiles, stream);
 }
 
 }  // namespace asd

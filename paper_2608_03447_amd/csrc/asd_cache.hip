@@ -25,15 +25,12 @@ struct Request {
 __device__ __forceinline__ Request request_of(const Blocks& b, int32_t i, int lane) {
     Request r;
     const int32_t k = b.block_lens[i];
-    r.count = (k > 0 ? k : 0) + 1;
+    r.count = rows_of_block(k);
     if (b.row_offsets) {
         r.row = b.row_offsets[i];
     } else {
         long long sum = 0;
-        for (int32_t j = lane; j < i; j += 64) {
-            const int32_t kj = b.block_lens[j];
-            sum += (kj > 0 ? kj : 0) + 1;
-        }
+        for (int32_t j = lane; j < i; j += 64) sum += rows_of_block(b.block_lens[j]);
         for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s);
         r.row = sum;
     }

@@ -33,6 +33,9 @@ struct Blocks {
 };
 
 #ifdef __HIPCC__
+// Rows of a block of K drafts (a K beyond any batch stays one that does not fit).
+__device__ __forceinline__ int32_t rows_of_block(int32_t k) { return min(max(k, 0), 0x7ffffffe) + 1; }
+
 // LDS written by one lane of a wavefront is read by another after this.
 __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -65,6 +68,10 @@ struct AttentionArgs {
     const uint64_t* mask;
     int32_t mask_words;
     void* out;
+    // t / page_size = (2 t page_magic / 2^32) >> page_shift for 0 <= t < 2^31: with 2^shift >=
+    // page_size and magic = ceil(2^(31 + shift) / page_size) the excess stays below 1 / page_size.
+    uint32_t page_magic;
+    int32_t page_shift;
 };
 size_t attention_workspace_bytes(int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                  int32_t num_requests, int64_t total_rows, int cus);

@@ -172,6 +172,15 @@ def test_requests_that_do_not_fit_are_skipped():
     assert asd.asd_device_error(clear=True) == asd.ASD_DEVERR_CACHE
 
 
+def test_workspaces_may_hold_anything():
+    """Stretches without work, and items that no stretch cuts, say so themselves."""
+    for lens, cached in (([0], [5]), ([8, 0, 16], [900, 3000, 100]), ([0] * 40, [700] * 40)):
+        b = Batch(lens, cached, 8, 2, 128, BF16, 16)
+        q = queries(b)
+        size = asd.asd_block_attention_workspace_bytes(8, 2, 128, b.n, b.rows)
+        check_attention(b, q, workspace=torch.full((size,), 0x5a, dtype=torch.uint8, device=DEV))
+
+
 def test_a_cache_past_32_bits():
     """Pages 2^31 elements and more into the cache, through strides that leave holes."""
     stride = 1 << 23
