@@ -536,7 +536,7 @@ asd_status asd_rope_append(const void *q, const void *k, const void *v, asd_dtyp
  * q               row r's heads, dense, at q + r * q_stride (elements, a multiple
  *                 of 8); dtype ASD_BF16 or ASD_F16; 16-byte aligned.
  * num_q_heads     a positive multiple of cache->num_heads, at most 65,536; times
- *                 total_rows / cache->num_heads below 2^31.
+ *                 total_rows below 2^31.
  * scale           finite.
  * cache           head_dim 64, 128 or 256.
  * mask            uint64 [total_rows][mask_words], or NULL with mask_words = 0.

@@ -22,6 +22,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / 64;
 constexpr int kStrip = 32;                          // tokens a wavefront takes at a time
 constexpr int kUnit = kStrip * kAttendWaves;
+constexpr int32_t kMostTeam = 32;
 
 // The same value in every lane, in scalar registers.
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -46,6 +47,7 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
 // Where a workgroup's stretch begins.
 struct Where {
     int64_t id;         // the stretch, -1: there is none for this workgroup
+    int32_t member;     // which of the stretch's workgroups this is
     int64_t per;        // units a stretch; the last one may have fewer
     int64_t total;      // units of the batch
     int64_t unit;       // the stretch's first unit, counted within its request
@@ -55,15 +57,15 @@ struct Where {
 };
 
 template <int kRows>
-__device__ __forceinline__ int64_t units_of(const Blocks& b, int32_t group, int64_t row, int32_t count,
+__device__ __forceinline__ int64_t units_of(const Blocks& b, int32_t group, int32_t team, int64_t row, int32_t count,
                                             int64_t cached, uint32_t& err) {
     const int64_t room = (int64_t)b.cache.max_pages * b.cache.page_size;
     const bool rows_ok = row >= 0 && row <= b.total_rows - count;
     const bool cache_ok = cached >= 0 && cached <= room - count;
     err |= (rows_ok ? 0u : kDecodeErrRows) | (cache_ok ? 0u : kDecodeErrCache);
     if (!rows_ok || !cache_ok) return 0;
-    const int64_t tiles = ((int64_t)count * group + kRows - 1) / kRows;
-    return tiles * b.cache.num_heads * ((cached + count + kUnit - 1) / kUnit);
+    const int32_t tiles = (count * group + kRows - 1) / kRows, rounds = (tiles + team - 1) / team;
+    return (int64_t)rounds * b.cache.num_heads * ((cached + count + kUnit - 1) / kUnit);
 }
 
 // Sum of v over the threads before this one, and over all of them.
@@ -91,7 +93,7 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* box, int64_t* 
 // The workgroup's stretch: every thread sums its share of the requests (one, up to 256 requests),
 // and the one whose share holds the stretch's first unit says where it is.
 template <int kRows>
-__device__ __forceinline__ Where locate(const Blocks& b, int32_t group, int64_t* box, Where* out) {
+__device__ __forceinline__ Where locate(const Blocks& b, int32_t group, int32_t team, int64_t* box, Where* out) {
     const int32_t n = b.num_requests, per_thread = (n + kAttendThreads - 1) / kAttendThreads;
     const int32_t first = min(n, (int32_t)threadIdx.x * per_thread), last = min(n, first + per_thread);
     int64_t row = 0, unused, mine = 0;
@@ -106,27 +108,29 @@ __device__ __forceinline__ Where locate(const Blocks& b, int32_t group, int64_t*
     for (int32_t i = first; i < last; ++i) {
         const int32_t k = i == first ? k0 : b.block_lens[i], count = rows_of_block(k);
         err |= k < 0 ? kDecodeErrNegativeK : 0u;
-        units += units_of<kRows>(b, group, b.row_offsets ? b.row_offsets[i] : at, count,
+        units += units_of<kRows>(b, group, team, b.row_offsets ? b.row_offsets[i] : at, count,
                                  i == first ? c0 : b.cache_lens[i], err);
         at += count;
     }
     if (blockIdx.x == 0 && err != 0) atomicOr(b.error_word, err);
     int64_t total;
     int64_t before = block_scan(units, box, &total);
-    // Equal stretches, the last one short.  Workgroups go to the XCDs in turn; neighbouring
-    // stretches, which may share keys and values, go to one of them.
-    const int64_t wgs = gridDim.x, per = total <= wgs ? 1 : quotient(total + wgs - 1, wgs);
-    const int64_t used = per == 1 ? total : quotient(total + per - 1, per), eighth = (used + 7) / 8;
-    const int64_t id = (int64_t)(blockIdx.x & 7) * eighth + (blockIdx.x >> 3), unit = id * per;
-    if ((int64_t)(blockIdx.x >> 3) >= eighth || id >= used) return Where{-1, 0, 0, 0, 0, 0, 0, 0};
+    // Equal stretches, the last one short.  Workgroups go to the XCDs in turn; those of a stretch,
+    // which read the same keys and values, go to one of them, and so do neighbouring stretches.
+    const int64_t most = gridDim.x / team, per = total <= most ? 1 : quotient(total + most - 1, most);
+    const int32_t used = (int32_t)(per == 1 ? total : quotient(total + per - 1, per)) * team, eighth = (used + 7) / 8;
+    const int32_t worker = (int32_t)(blockIdx.x & 7) * eighth + (int32_t)(blockIdx.x >> 3);
+    if ((int32_t)(blockIdx.x >> 3) >= eighth || worker >= used) return Where{-1, 0, 0, 0, 0, 0, 0, 0, 0};
+    const int32_t id = worker / team;
+    const int64_t unit = id * per;
     if (unit >= before && unit < before + units) {
         for (int32_t i = first; i < last; ++i) {
             const int32_t count = rows_of_block(i == first ? k0 : b.block_lens[i]);
             const int64_t cached = i == first ? c0 : b.cache_lens[i];
             const int64_t at_row = b.row_offsets ? b.row_offsets[i] : row;
-            const int64_t u = units_of<kRows>(b, group, at_row, count, cached, err);
+            const int64_t u = units_of<kRows>(b, group, team, at_row, count, cached, err);
             if (unit < before + u) {
-                *out = Where{id, per, total, unit - before, at_row, cached, i, count};
+                *out = Where{id, worker - id * team, per, total, unit - before, at_row, cached, i, count};
                 break;
             }
             before += u;
@@ -134,7 +138,7 @@ __device__ __forceinline__ Where locate(const Blocks& b, int32_t group, int64_t*
         }
     }
     __syncthreads();
-    return Where{uniform(out->id),  uniform(out->per),    uniform(out->total),   uniform(out->unit),
+    return Where{uniform(out->id),   uniform(out->member), uniform(out->per),    uniform(out->total),  uniform(out->unit),
                  uniform(out->row), uniform(out->cached), uniform(out->request), uniform(out->count)};
 }
 
@@ -142,7 +146,7 @@ __device__ __forceinline__ Where locate(const Blocks& b, int32_t group, int64_t*
 // workgroup writes one, those without a stretch too, since nothing else clears them.
 struct alignas(32) Cut {
     int64_t row;        // the request's first row
-    int32_t id;         // the stretch
+    int32_t worker;     // stretch and workgroup of it, counted through
     int32_t head, first, pairs;
     int32_t parts;      // stretches that hold a part of the item, 0: it is not cut here
 };
@@ -214,19 +218,24 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
 
     const asd_paged_cache& cache = a.b.cache;
     const int32_t group = a.num_q_heads / cache.num_heads;
-    Where at = locate<kRows>(a.b, group, box, &where_box);
+    Where at = locate<kRows>(a.b, group, a.team, box, &where_box);
     if (at.id < 0) {
         if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{0, 0, 0, 0, 0, 0};
         return;
     }
     int64_t left = min(at.per, at.total - at.id * at.per);
-    const float per = __uint_as_float((uint32_t)uniform((int32_t)__float_as_uint(a.scale * 1.44269504f)));
+    const int64_t worker = at.id * a.team + at.member;
+    bool cut = false;
+    // Scores enter as scale > 0: a negative scale turns the queries' signs, a zero one makes them zeros.
+    const float per = __uint_as_float((uint32_t)uniform((int32_t)__float_as_uint(
+        a.scale == 0.0f ? 1.0f : fabsf(a.scale) * 1.44269504f)));
+    const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u, keep_q = a.scale == 0.0f ? 0u : ~0u;
 
     while (left > 0) {
         const int32_t count = at.count;
         const int64_t cached64 = at.cached;
         uint32_t unused = 0;
-        if (units_of<kRows>(a.b, group, at.row, count, cached64, unused) <= at.unit) {
+        if (units_of<kRows>(a.b, group, a.team, at.row, count, cached64, unused) <= at.unit) {
             // on to the next request
             at.row = a.b.row_offsets ? uniform(a.b.row_offsets[at.request + 1]) : at.row + count;
             at.request += 1;
@@ -239,10 +248,18 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
         const int64_t units = (cached64 + count + kUnit - 1) / kUnit;
         const int64_t item = quotient(at.unit, units), from = at.unit - item * units;
         const int64_t to = from + left < units ? from + left : units;
-        const int32_t head = (int32_t)quotient(item, tiles);
-        const int32_t first = (int32_t)(item - (int64_t)head * tiles) * kRows;      // of the pairs
+        const int32_t rounds = (tiles + a.team - 1) / a.team, head = (int32_t)item / rounds;
+        const int32_t mine = ((int32_t)item - head * rounds) * a.team + at.member, first = mine * kRows;      // of the pairs
         at.unit += to - from;
         left -= to - from;
+        if (mine >= tiles) continue;
+        const bool complete = from == 0 && to == units;
+        if (from == 0 && !complete) {           // the stretch ends here
+            cut = true;
+            if (threadIdx.x == 0)
+                cuts[blockIdx.x] = Cut{at.row, (int32_t)worker, head, first, pairs,
+                                       1 + (int32_t)quotient(units - to + at.per - 1, at.per)};
+        }
 
         const int tid = fresh(threadIdx.x), lane = tid & 63, wave = uniform(tid >> 6), n = lane & 15, g = lane >> 4;
         // the tile's queries: B operands, lane n's row, 8 elements of every 32
@@ -250,8 +267,9 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
             const int32_t m = first + 16 * tile + n;
             if (m >= pairs) return x8{};
             const int32_t p = m / group;
-            return *(const x8*)((const T*)a.q + (at.row + p) * a.q_stride +
-                                (head * group + m - p * group) * D + 32 * step + 8 * g);
+            const u32x4 x = *(const u32x4*)((const T*)a.q + (at.row + p) * a.q_stride +
+                                            (head * group + m - p * group) * D + 32 * step + 8 * g);
+            return __builtin_bit_cast(x8, (x ^ flip) & keep_q);
         };
         x8 q[kQueriesInLds ? 1 : kTiles][kSteps];
         __syncthreads();
@@ -329,41 +347,57 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
                 }
             }
         };
-        // Scores and weights of tile `tile`, whose lane sees the tokens of `seen` (8 bits).
+        // Scores and weights of a strip; a lane's row of tile i sees the tokens of bits 8 i.. of `seen`.
         x8 w[kTiles];
-        const auto weigh = [&](int tile, bool all, uint32_t seen) {
-            f32x4 s[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
+        const auto weigh = [&](bool all, uint32_t seen) {
+            f32x4 s[kTiles][2];
 #pragma unroll
-            for (int step = 0; step < kSteps; ++step) {
-                x8 qq;
-                if constexpr (kQueriesInLds) qq = queries[(tile * kSteps + step) * 64 + lane];
-                else qq = q[tile][step];
+            for (int tile = 0; tile < kTiles; ++tile) s[tile][0] = s[tile][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
-                for (int h = 0; h < 2; ++h) s[h] = Half<T>::mfma(k[h][step], qq, s[h]);
+            for (int step = 0; step < kSteps; ++step)
+#pragma unroll
+                for (int tile = 0; tile < kTiles; ++tile) {
+                    x8 qq;
+                    if constexpr (kQueriesInLds) qq = queries[(tile * kSteps + step) * 64 + lane];
+                    else qq = q[tile][step];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) s[tile][h] = Half<T>::mfma(k[h][step], qq, s[tile][h]);
+                }
+            float top[kTiles];
+            bool moves = false;
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile) {
+                if (!all) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (!((seen >> (8 * tile + j)) & 1)) s[tile][j >> 2][j & 3] = -INFINITY;
+                }
+                const f32x4 a = s[tile][0], b = s[tile][1];
+                top[tile] = rows_max(fmaxf(fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)),
+                                           fmaxf(fmaxf(b.x, b.y), fmaxf(b.z, b.w)))) * per;
+                moves |= top[tile] > ref[tile] + kLead;
             }
-            float x[8];
+            if (__any(moves)) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] = s[j >> 2][j & 3] * per;
-                if (!all) x[j] = (seen >> j) & 1 ? x[j] : -INFINITY;
+                for (int tile = 0; tile < kTiles; ++tile) {
+                    const float now = top[tile] > ref[tile] + kLead ? top[tile] - kSet : ref[tile];
+                    const float keep = now == ref[tile] ? 1.0f : __builtin_amdgcn_exp2f(ref[tile] - now);
+                    ref[tile] = now;
+                    sum[tile] *= keep;
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) o[tile][c] *= keep;
+                }
             }
-            float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])),
-                              fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            top = rows_max(top);
-            if (__any(top > ref[tile] + kLead)) {
-                const float now = top > ref[tile] + kLead ? top - kSet : ref[tile];
-                const float keep = now == ref[tile] ? 1.0f : __builtin_amdgcn_exp2f(ref[tile] - now);
-                ref[tile] = now;
-                sum[tile] *= keep;
 #pragma unroll
-                for (int c = 0; c < NC; ++c) o[tile][c] *= keep;
-            }
-            const float from_ref = ref[tile] == -INFINITY ? 0.0f : ref[tile];
+            for (int tile = 0; tile < kTiles; ++tile) {
+                const float from_ref = ref[tile] == -INFINITY ? 0.0f : ref[tile];
+                float x[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] = __builtin_amdgcn_exp2f(x[j] - from_ref);
-                sum[tile] += x[j];
-                w[tile][j] = (T)x[j];
+                for (int j = 0; j < 8; ++j) {
+                    x[j] = __builtin_amdgcn_exp2f(fmaf(s[tile][j >> 2][j & 3], per, -from_ref));
+                    w[tile][j] = (T)x[j];
+                }
+                sum[tile] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
             }
         };
         const auto add_values = [&]() {
@@ -396,11 +430,7 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
                 asm volatile("" ::: "memory");
                 do {
                     valid = put_offsets(strip + kUnit, page);
-#pragma unroll
-                    for (int tile = 0; tile < kTiles; ++tile) {
-                        weigh(tile, true, 0);
-                        if (kTiles > 2) __builtin_amdgcn_sched_barrier(0);
-                    }
+                    weigh(true, 0);
                     page = page_of(strip + 2 * kUnit);
                     load_keys();
                     __builtin_amdgcn_sched_barrier(0);
@@ -435,8 +465,7 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
                     seen |= (uint32_t)sees << (8 * tile + j);
                 }
             }
-#pragma unroll
-            for (int tile = 0; tile < kTiles; ++tile) weigh(tile, false, seen >> (8 * tile));
+            weigh(false, seen);
 
             // Values that are not there are zeros.  A token that holds an infinity or a NaN
             // would reach every row through its weight 0: it leaves the product and is added by
@@ -497,8 +526,7 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
 
         // the wavefronts' sums, joined tile by tile
         const int tid_end = fresh(tid), n_end = tid_end & 15, g_end = tid_end >> 4 & 3, row = tid_end >> 4;
-        const bool complete = from == 0 && to == units;
-        float* const slot = partials + (2 * at.id + (from > 0 ? 0 : 1)) * (int64_t)(kRows * (D + 2));
+        float* const slot = partials + (2 * worker + (from > 0 ? 0 : 1)) * (int64_t)(kRows * (D + 2));
         #pragma unroll
         for (int tile = 0; tile < kTiles; ++tile) {
             sum[tile] = rows_sum(sum[tile]);
@@ -552,10 +580,8 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
             }
         }
         __syncthreads();
-        if (tid_end == 0 && left == 0)
-            cuts[blockIdx.x] = Cut{at.row, (int32_t)at.id, head, first, pairs,
-                              from == 0 && !complete ? 1 + (int32_t)quotient(units - to + at.per - 1, at.per) : 0};
     }
+    if (threadIdx.x == 0 && !cut) cuts[blockIdx.x] = Cut{0, 0, 0, 0, 0, 0};
 }
 
 // Joins the partials of the item that is cut by the end of workgroup blockIdx.x's stretch, if one is; a
@@ -573,9 +599,9 @@ __global__ __launch_bounds__(kAttendThreads) void asd_attend_join_kernel(Attenti
     const int lane = threadIdx.x & 63, wave = uniform((int32_t)threadIdx.x >> 6);
     const Cut cut = cuts[blockIdx.x];
     if (cut.parts == 0) return;
-    const int64_t id = cut.id;
+    const int64_t worker = cut.worker;
     const int32_t group = a.num_q_heads / a.b.cache.num_heads;
-    const auto part = [&](int j) { return partials + (2 * (id + j) + (j == 0 ? 1 : 0)) * kSize; };
+    const auto part = [&](int j) { return partials + (2 * (worker + (int64_t)j * a.team) + (j == 0 ? 1 : 0)) * kSize; };
     const auto row_of = [&](int32_t m) {
         const int32_t p = m / group;
         return (T*)a.out + ((cut.row + p) * a.num_q_heads + cut.head * group + m - p * group) * D;
@@ -671,6 +697,14 @@ int tiles_of(int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_
     return (int)((tiles + items - 1) / items);
 }
 
+// Workgroups of a stretch: one for every tile of an average block, all of which read its keys and
+// values at the same time, up to those that an XCD holds.
+int32_t team_of(int32_t num_q_heads, int32_t num_kv_heads, int32_t num_requests, int64_t total_rows, int tiles) {
+    const int64_t pairs = (total_rows + num_requests - 1) / num_requests * (num_q_heads / num_kv_heads);
+    const int64_t items = (pairs + 16 * tiles - 1) / (16 * tiles);
+    return (int32_t)(items < kMostTeam ? items : kMostTeam);
+}
+
 size_t partial_bytes(int64_t wgs, int head_dim, int tiles) {
     return (size_t)(2 * wgs) * 16 * tiles * (head_dim + 2) * sizeof(float);
 }
@@ -725,6 +759,7 @@ hipError_t launch_block_attention(const AttentionArgs& a, bool bf16, void* works
     b.page_magic = (uint32_t)((((uint64_t)1 << (31 + b.page_shift)) + c.page_size - 1) / c.page_size);
     const int tiles = tiles_of(a.num_q_heads, c.num_heads, c.head_dim, a.b.num_requests, a.b.total_rows);
     const int64_t wgs = (int64_t)cus * resident(c.head_dim, tiles);
+    b.team = team_of(a.num_q_heads, c.num_heads, a.b.num_requests, a.b.total_rows, tiles);
     return bf16 ? attend_any<__bf16>(b, workspace, wgs, tiles, stream)
                 : attend_any<_Float16>(b, workspace, wgs, tiles, stream);
 }

@@ -72,6 +72,7 @@ struct AttentionArgs {
     // page_size and magic = ceil(2^(31 + shift) / page_size) the excess stays below 1 / page_size.
     uint32_t page_magic;
     int32_t page_shift;
+    int32_t team;          // workgroups that share a stretch
 };
 size_t attention_workspace_bytes(int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                  int32_t num_requests, int64_t total_rows, int cus);

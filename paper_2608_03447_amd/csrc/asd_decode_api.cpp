@@ -143,7 +143,7 @@ asd_status asd_block_attention(const void* q, asd_dtype dtype, int64_t q_stride,
         return ASD_EINVAL;
     if (bad_heads(num_q_heads, cache->num_heads, cache->head_dim) || !std::isfinite(scale))
         return ASD_EINVAL;
-    if (total_rows * (num_q_heads / cache->num_heads) >= k2G) return ASD_EINVAL;
+    if (total_rows * num_q_heads >= k2G) return ASD_EINVAL;
     if (mask_words < 0 || (mask != nullptr) != (mask_words > 0)) return ASD_EINVAL;
     if (workspace && ((uintptr_t)workspace & 255) != 0) return ASD_EINVAL;
     if (num_requests == 0) return ASD_OK;
