@@ -169,8 +169,15 @@ template <> struct Half<_Float16> {
     static constexpr uint32_t kExponent = 0x7c00u;
 };
 
-// Workgroups that fit on a compute unit, by their registers.
-constexpr int resident(int head_dim, int tiles) { return head_dim == 256 ? 1 : tiles == 1 ? 3 : 2; }
+// Workgroups that fit on a compute unit, by their registers and LDS.
+constexpr int resident(int head_dim, int tiles) { return head_dim == 256 ? 1 : head_dim == 64 && tiles == 1 ? 3 : 2; }
+
+// 64 lanes' 16 bytes each to LDS, from `lds` on; counted by vmcnt and waited for by the caller.
+// (In asm since the compiler takes the builtin to write one lane's bytes alone and moves reads of
+// the others' past it.  The s_nop: it does not see the address or m0 as just written.)
+__device__ __forceinline__ void copy_to_lds(const char* src, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(src) : "memory");
+}
 
 // The greatest / the sum over the four lanes that hold one query row (lanes l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float rows_max(float x) {
@@ -210,8 +217,13 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
     typedef typename Half<T>::x8 x8;
     __shared__ int64_t box[kAttendWaves];
     __shared__ Where where_box;
-    __shared__ int64_t offsets[kAttendWaves][kStrip];
-    __shared__ float joined[kAttendWaves][16][D + 4];
+    __shared__ int64_t offsets[kAttendWaves][2][kStrip];
+    // a wavefront's keys of two strips; its rows of the join at an item's end
+    constexpr int kKeyBytes = kStrip * D * 2;
+    __shared__ __align__(16) char region[kAttendWaves][2 * kKeyBytes];
+    float(*const joined)[sizeof(region[0]) / 4] = (float(*)[sizeof(region[0]) / 4])region;
+    constexpr int kPitch = D + 4;
+    static_assert(16 * kPitch * 4 <= 2 * kKeyBytes, "the join's rows fit");
     __shared__ float tops[kAttendWaves][16], sums[kAttendWaves][16];
     __shared__ int32_t row_p[kRows];                  // the block's row of every row of the tile
     __shared__ x8 queries[kQueriesInLds ? kTiles * kSteps * 64 : 1];
@@ -302,10 +314,8 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
         const int32_t end = a.mask ? end_all : cached + last_p + 1;
         const int32_t strip_end = (int32_t)min(to * kUnit, (int64_t)end);
         int32_t strip = (int32_t)(from * kUnit) + wave * kStrip;
-        int64_t* const offs = offsets[wave];
         const int32_t* const table = cache.page_table + (int64_t)at.request * cache.max_pages;
-        // at the lane's part of a token: 8 elements of every 32 of its key, D / 16 of its value
-        const char* const keys = (const char*)((const T*)cache.keys + (int64_t)head * cache.head_stride + 8 * g);
+        const char* const keys = (const char*)((const T*)cache.keys + (int64_t)head * cache.head_stride ); 
         const char* const values = (const char*)((const T*)cache.values + (int64_t)head * cache.head_stride + NC * n);
 
         // A strip's page ids (lanes l and l + 32 hold token l; tokens behind the last one take
@@ -313,30 +323,40 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
         // are there, the others' offsets being 0.
         const auto page_at = [&](int32_t t) { return (int32_t)(__umulhi(2 * (uint32_t)t, a.page_magic) >> a.page_shift); };
         const auto page_of = [&](int32_t t0) -> int32_t { return table[page_at(min(t0 + (lane & 31), end_all - 1))]; };
-        const auto put_offsets = [&](int32_t t0, int32_t page) -> uint32_t {
+        const auto put_offsets = [&](int b, int32_t t0, int32_t page) -> uint32_t {
             const int32_t t = t0 + (lane & 31);
             const bool ok = t < end_all && (uint32_t)page < (uint32_t)cache.num_pages;
             const int32_t slot = t - page_at(t) * cache.page_size;
             const int64_t off = ((int64_t)page * cache.page_stride + (int64_t)slot * cache.token_stride) * 2;
             wave_sync();
-            if (lane < 32) offs[lane] = ok ? off : 0;
+            if (lane < 32) offsets[wave][b][lane] = ok ? off : 0;
             wave_sync();
             return (uint32_t)__ballot(ok);
         };
-        x8 k[2][kSteps];
         u32x4 v[8][kVecs];
-        const auto load_keys = [&]() {
+        // Keys go to LDS as they lie in memory, D / 8 lanes a token, so that 16 lanes read whole lines
+        // (16 tokens' pieces of 16 bytes, as the operand wants them, cost the L1 64 lookups an instruction:
+        // 64 single tokens over up to 8,192 took 226 us); a token's pieces of 16 bytes are
+        // turned by its number, so that the operand's reads of 16 tokens meet no bank twice.
+        constexpr int kLanes = D / 8, kAtOnce = 64 / kLanes, kTurn = D == 64 ? 1 : 0, kTurns = D == 64 ? 7 : 15;
+        const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)region[wave];
+        const auto load_keys = [&](int b) {
+            const int r0 = lane / kLanes, piece = lane % kLanes;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const char* src = keys + offs[16 * h + n];
-#pragma unroll
-                for (int step = 0; step < kSteps; ++step) k[h][step] = *(const x8*)(src + 64 * step);
+            for (int i = 0; i < kStrip / kAtOnce; ++i) {
+                const int r = kAtOnce * i + r0;
+                copy_to_lds(keys + offsets[wave][b][r] + 16 * (piece ^ (r >> kTurn & kTurns)),
+                            lds + b * kKeyBytes + 1024 * i);
             }
         };
-        const auto load_values = [&]() {
+        const auto key = [&](int b, int h, int step) -> x8 {
+            return *(const x8*)(region[wave] + b * kKeyBytes + (16 * h + n) * (2 * D) +
+                                16 * ((4 * step + g) ^ (n >> kTurn & kTurns)));
+        };
+        const auto load_values = [&](int b) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const char* src = values + offs[(j & 3) + 4 * g + 16 * (j >> 2)];
+                const char* src = values + offsets[wave][b][(j & 3) + 4 * g + 16 * (j >> 2)];
                 if constexpr (NC == 4) {
                     const u32x2 w = *(const u32x2*)src;
                     v[j][0].x = w.x;
@@ -349,20 +369,22 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
         };
         // Scores and weights of a strip; a lane's row of tile i sees the tokens of bits 8 i.. of `seen`.
         x8 w[kTiles];
-        const auto weigh = [&](bool all, uint32_t seen) {
+        const auto weigh = [&](int b, bool all, uint32_t seen) {
             f32x4 s[kTiles][2];
 #pragma unroll
             for (int tile = 0; tile < kTiles; ++tile) s[tile][0] = s[tile][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int step = 0; step < kSteps; ++step)
+            for (int step = 0; step < kSteps; ++step) {
+                const x8 k[2] = {key(b, 0, step), key(b, 1, step)};
 #pragma unroll
                 for (int tile = 0; tile < kTiles; ++tile) {
                     x8 qq;
                     if constexpr (kQueriesInLds) qq = queries[(tile * kSteps + step) * 64 + lane];
                     else qq = q[tile][step];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) s[tile][h] = Half<T>::mfma(k[h][step], qq, s[tile][h]);
+                    for (int h = 0; h < 2; ++h) s[tile][h] = Half<T>::mfma(k[h], qq, s[tile][h]);
                 }
+            }
             float top[kTiles];
             bool moves = false;
 #pragma unroll
@@ -372,9 +394,9 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
                     for (int j = 0; j < 8; ++j)
                         if (!((seen >> (8 * tile + j)) & 1)) s[tile][j >> 2][j & 3] = -INFINITY;
                 }
-                const f32x4 a = s[tile][0], b = s[tile][1];
-                top[tile] = rows_max(fmaxf(fmaxf(fmaxf(a.x, a.y), fmaxf(a.z, a.w)),
-                                           fmaxf(fmaxf(b.x, b.y), fmaxf(b.z, b.w)))) * per;
+                const f32x4 x = s[tile][0], y = s[tile][1];
+                top[tile] = rows_max(fmaxf(fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)),
+                                           fmaxf(fmaxf(y.x, y.y), fmaxf(y.z, y.w)))) * per;
                 moves |= top[tile] > ref[tile] + kLead;
             }
             if (__any(moves)) {
@@ -414,58 +436,64 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
             }
         };
 
-        // Strips that every row sees whole.  The next strip's keys are loaded once this one's are
-        // used, its values likewise, and the page ids of the one after it a strip ahead, so that
-        // no load is waited for where it is issued.
-        uint32_t valid = 0;
+        // While a strip's scores are formed, its values and the next strip's keys are on the way, and
+        // the page ids of the one after it.  Loads return in order and the next keys are
+        // asked for before this strip's values, so that they are in once these are used, with no wait
+        // of their own.  (Strips behind the last one load what offset 0 holds, for nothing.)
+        uint32_t valid = 0, ahead = 0;
+        int b = 0;
         if (strip < strip_end) {
-            valid = put_offsets(strip, page_of(strip));
-            if (valid == ~0u && strip + kStrip <= cached) {
-                int32_t page = page_of(strip + kUnit);
-                __builtin_amdgcn_sched_barrier(0);      // the order of the loop, so that its waits are short
-                load_keys();
-                __builtin_amdgcn_sched_barrier(0);
-                load_values();
-                // (the loads stay here: sunk into the loop they would not run ahead)
-                asm volatile("" ::: "memory");
-                do {
-                    valid = put_offsets(strip + kUnit, page);
-                    weigh(true, 0);
-                    page = page_of(strip + 2 * kUnit);
-                    load_keys();
-                    __builtin_amdgcn_sched_barrier(0);
-                    add_values();
-                    __builtin_amdgcn_sched_barrier(0);
-                    load_values();
-                    asm volatile("" ::: "memory");
-                    strip += kUnit;
-                } while (strip < strip_end && valid == ~0u && strip + kStrip <= cached);
-            }
+            const int32_t page = page_of(strip), next = page_of(strip + kUnit);
+            valid = put_offsets(0, strip, page);
+            load_keys(0);
+            ahead = put_offsets(1, strip + kUnit, next);
+            load_keys(1);
+            load_values(0);
+            asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kStrip / kAtOnce + 8 * kVecs) : "memory");
+        }
+        // Strips that every row sees whole.
+        while (strip < strip_end && valid == ~0u && strip + kStrip <= cached) {
+            const int32_t after = page_of(strip + 2 * kUnit);
+            weigh(b, true, 0);
+            add_values();
+            asm volatile("s_waitcnt vmcnt(1)" ::: "memory");       // all but `after`: waited for by its uses already
+            strip += kUnit;
+            valid = ahead;
+            ahead = put_offsets(b, strip + kUnit, after);
+            load_keys(b);
+            b ^= 1;
+            load_values(b);
         }
         // The others: the block's own tokens, the strip that the sequence ends in, bad pages.
 #pragma unroll 1
         while (strip < strip_end) {
             if (lane < 32 && strip + lane < end_all && !((valid >> lane) & 1))
                 atomicOr(a.b.error_word, kDecodeErrCache);
-            load_keys();
-            load_values();
-            // which of the lane's 8 tokens its rows see, 8 bits a tile, and which are there at all
-            uint32_t seen = 0, there = 0;
-#pragma unroll 1
-            for (int j = 0; j < 8; ++j) {
-                const int32_t at_strip = (j & 3) + 4 * g + 16 * (j >> 2), x = strip + at_strip - cached;
-                if (!((valid >> at_strip) & 1)) continue;
-                there |= 1u << j;
-#pragma unroll 1
-                for (int tile = 0; tile < kTiles; ++tile) {
-                    const int32_t p = row_p[16 * tile + n];
-                    const bool sees = x < 0 || (!a.mask ? x <= p
-                                                        : x < 64 * (int64_t)a.mask_words &&
-                        ((a.mask[(at.row + p) * a.mask_words + x / 64] >> (x % 64)) & 1) != 0);
-                    seen |= (uint32_t)sees << (8 * tile + j);
+            // the tokens that each tile's row sees, a bit each: cached ones, and the block's by the mask
+            uint32_t window[kTiles];
+            const int32_t past = strip - cached;         // the block's first token; negative: before it
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile) {
+                const int32_t p = row_p[16 * tile + n];
+                if (a.mask) {
+                    const uint64_t* const words = a.mask + (at.row + p) * a.mask_words;
+                    const int32_t x = max(past, 0), at_word = x >> 6, bit = x & 63;
+                    uint64_t bits = 0;
+                    if (at_word < a.mask_words) bits = words[at_word] >> bit;
+                    if (bit > 32 && at_word + 1 < a.mask_words) bits |= words[at_word + 1] << (64 - bit);
+                    const int32_t before = min(max(-past, 0), 32);
+                    window[tile] = (uint32_t)(bits << before) | (uint32_t)((1ull << before) - 1);
+                } else {
+                    window[tile] = (uint32_t)((1ull << min(max(p + 1 - past, 0), 32)) - 1);
                 }
             }
-            weigh(false, seen);
+            // of the lane's 8 tokens: which its rows see, 8 bits a tile, and which are there at all
+            const auto mine = [&](uint32_t x) { return (x >> (4 * g) & 0xf) | (x >> (16 + 4 * g) & 0xf) << 4; };
+            const uint32_t there = mine(valid);
+            uint32_t seen = 0;
+#pragma unroll
+            for (int tile = 0; tile < kTiles; ++tile) seen |= mine(window[tile] & valid) << (8 * tile);
+            weigh(b, false, seen);
 
             // Values that are not there are zeros.  A token that holds an infinity or a NaN
             // would reach every row through its weight 0: it leaves the product and is added by
@@ -497,21 +525,23 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
                 }
             }
             add_values();
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             if (odd != 0) {
+                float* const special_weights = (float*)(region[wave] + b * kKeyBytes);     // its keys are used
 #pragma unroll
                 for (int tile = 0; tile < kTiles; ++tile) {
                     wave_sync();
 #pragma unroll
                     for (int j = 0; j < 8; ++j)       // -1: not seen
-                        joined[wave][n][(j & 3) + 4 * g + 16 * (j >> 2)] =
+                        special_weights[n * (kStrip + 1) + (j & 3) + 4 * g + 16 * (j >> 2)] =
                             (seen >> (8 * tile + j)) & 1 ? (float)w[tile][j] : -1.0f;
                     wave_sync();
 #pragma unroll 1
                     for (uint32_t rest = odd; rest != 0; rest &= rest - 1) {
                         const int32_t at_strip = __builtin_ctz(rest);
-                        const float weight = joined[wave][n][at_strip];
+                        const float weight = special_weights[n * (kStrip + 1) + at_strip];
                         if (weight == -1.0f) continue;
-                        const T* src = (const T*)(values - 2 * NC * n + offs[at_strip]) + 4 * NC * g;
+                        const T* src = (const T*)(values - 2 * NC * n + offsets[wave][b][at_strip]) + 4 * NC * g;
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -521,8 +551,16 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
                 }
             }
             strip += kUnit;
-            if (strip < strip_end) valid = put_offsets(strip, page_of(strip));
+            valid = ahead;
+            if (strip < strip_end) {
+                ahead = put_offsets(b, strip + kUnit, page_of(strip + kUnit));
+                load_keys(b);
+            }
+            b ^= 1;
+            if (strip < strip_end) load_values(b);
         }
+        // (keys loaded ahead for nothing have to be in before their place is used again)
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
         // the wavefronts' sums, joined tile by tile
         const int tid_end = fresh(tid), n_end = tid_end & 15, g_end = tid_end >> 4 & 3, row = tid_end >> 4;
@@ -545,7 +583,7 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
             for (int r = 0; r < 4; ++r)
                 #pragma unroll
                 for (int c = 0; c < NC; c += 4)
-                    *(f32x4*)&joined[wave][n_end][4 * NC * g_end + NC * r + c] =
+                    *(f32x4*)&joined[wave][n_end * kPitch + 4 * NC * g_end + NC * r + c] =
                         f32x4{o[tile][c][r], o[tile][c + 1][r], o[tile][c + 2][r], o[tile][c + 3][r]} * mine;
             __syncthreads();
             // 16 threads a row, each every 16th vector of 4 elements
@@ -558,19 +596,20 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
                 total += tops[w][row] == -INFINITY ? 0.0f
                                                    : sums[w][row] * __builtin_amdgcn_exp2f(tops[w][row] - best);
             const int32_t m = first + 16 * tile + row;
-            if (!complete && n_end == 0) {
+            if (!complete && n_end == 0 && m < pairs) {
                 slot[kRows * D + 16 * tile + row] = best;
                 slot[kRows * (D + 1) + 16 * tile + row] = total;
             }
             const int32_t p = row_p[16 * tile + row];
             const float over = best == -INFINITY ? 0.0f : 1.0f / total;
             for (int e = 4 * n_end; e < D; e += 64) {
-                f32x4 x = *(const f32x4*)&joined[0][row][e];
+                f32x4 x = *(const f32x4*)&joined[0][row * kPitch + e];
                 #pragma unroll
-                for (int w = 1; w < kAttendWaves; ++w) x += *(const f32x4*)&joined[w][row][e];
+                for (int w = 1; w < kAttendWaves; ++w) x += *(const f32x4*)&joined[w][row * kPitch + e];
+                if (m >= pairs) break;
                 if (!complete) {
                     *(f32x4*)&slot[(16 * tile + row) * D + e] = x;
-                } else if (m < pairs) {
+                } else {
                     T* dst = (T*)a.out + ((at.row + p) * a.num_q_heads + head * group + m - p * group) * D + e;
                     typename Half<T>::x2 y[2];
                     #pragma unroll
