@@ -1,4 +1,21 @@
 // gfx950 kernels that draw a token from every logit row.
+//
+// Pass 1 (asd_sample_scan_kernel) reads every row once from HBM, a wavefront a group
+// of 1,024 logits at a time, and leaves the greatest logit of every 64 (a
+// sub-block) and, for rows whose whole mass counts, the group's sum of
+// exp((z - its greatest) / T) in binary64.
+//
+// Pass 2 (asd_sample_pick_kernel), a workgroup a row, works on those: without filters the draw
+// falls into one group, which is read again; with them, a threshold that as many sub-block
+// maxima reach as tokens are wanted bounds the candidates from below, only the sub-blocks
+// whose maximum reaches it are read again, and the filters' cuts are found among the
+// candidates by bisection over the logits' keys.  Rows that keep too many tokens for that (a nucleus of
+// tens of thousands) are left to
+//
+// Pass 3 (asd_sample_flat_kernel): a histogram of the row's weights over its keys' leading bits gives the
+// bin that holds the cut, a second reading collects that bin and sums what lies above it.
+//
+// The running sum is taken in index order, so nothing is sorted.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -8,8 +25,10 @@ namespace asd {
 namespace {
 
 typedef unsigned long long u64;
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kGroup = 1024, kSub = 64, kSubs = kGroup / kSub;
 
 template <int kType> struct Element;
 template <> struct Element<ASD_F32> {
@@ -33,252 +52,926 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 }
 constexpr uint32_t kKeyNegInf = 0x007fffffu, kKeyNan = 0xffffffffu;
 
-template <typename V, typename Op>
-__device__ __forceinline__ V block_reduce(V v, Op op, V* box) {
-    for (int s = 32; s > 0; s >>= 1) v = op(v, (V)__shfl_xor(v, s));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) box[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = box[0];
-    for (int w = 1; w < kWaves; ++w) v = op(v, box[w]);
-    __syncthreads();
-    return v;
+// 2^x for x <= 0, to 2^-47: the Taylor polynomial of degree 11 of 2^r, |r| <= 1/2
+// (the next term is (ln 2 / 2)^12 / 12! = 6e-15).  2^0 is 1 exactly; below 2^-1000 it is 0.
+__device__ __forceinline__ double power2(double x) {
+    const bool none = x < -1000.0;
+    x = fmax(x, -1000.0);
+    const double n = rint(x), r = x - n;
+    double p = 4.4455382718708114e-10;                 // ln(2)^k / k!, k = 11 .. 1
+    p = fma(p, r, 7.0549116208011232e-09);
+    p = fma(p, r, 1.0178086009239700e-07);
+    p = fma(p, r, 1.3215486790144309e-06);
+    p = fma(p, r, 1.5252733804059840e-05);
+    p = fma(p, r, 1.5403530393381609e-04);
+    p = fma(p, r, 1.3333558146428443e-03);
+    p = fma(p, r, 9.6181291076284771e-03);
+    p = fma(p, r, 5.5504108664821580e-02);
+    p = fma(p, r, 2.4022650695910071e-01);
+    p = fma(p, r, 6.9314718055994531e-01);
+    p = fma(p, r, 1.0);
+    return none ? 0.0 : ldexp(p, (int)n);
 }
 
-// A row's weights, exp((z - max) / T) in units of 2^-bits.
+// A row's weights, exp((z - top) / T).
 struct Weights {
-    double top, per;       // max z; log2(e) / T
-    double unit;           // 2^bits
+    double top, per;       // log2(e) / T
     float top_f;
-    __device__ __forceinline__ double real(float z) const {
-        if (z == top_f) return 1.0;
-        if (z == -INFINITY || top_f == INFINITY) return 0.0;
-        return exp2(((double)z - top) * per);
+    __device__ __forceinline__ Weights(float greatest, float t)
+        : top((double)greatest), per(1.44269504088896340736 / (double)t), top_f(greatest) {}
+    __device__ __forceinline__ double operator()(float z) const {
+        const double w = power2(((double)z - top) * per);
+        return z == top_f ? 1.0 : z == -INFINITY || top_f == INFINITY ? 0.0 : w;
     }
-    __device__ __forceinline__ u64 fixed(double w) const { return (u64)(w * unit + 0.5); }
 };
 
-// ceil(f * total) of a float 0 <= f < 1 and an integer below 2^63, exactly.
-__device__ __forceinline__ u64 share_ceil(float f, u64 total) {
+// Row parameters.
+struct Row {
+    float t, p, m;
+    int32_t k;
+    bool greedy, by_count, by_mass, by_floor;
+    __device__ __forceinline__ Row(const SampleArgs& a, int64_t row) {
+        t = a.temperature ? a.temperature[row] : 1.0f;
+        k = a.top_k ? a.top_k[row] : 0;
+        p = a.top_p ? a.top_p[row] : 1.0f;
+        m = a.min_p ? a.min_p[row] : 0.0f;
+        greedy = !(t > 0.0f);
+        by_count = k > 0 && k < a.vocab;
+        by_mass = p < 1.0f;
+        by_floor = m > 0.0f;
+        m = m < 1.0f ? m : 1.0f;
+    }
+};
+
+// What pass 1 leaves of a row: keys of its sub-blocks' maxima, keys and sums of its groups.
+struct Stats {
+    uint32_t* subs;        // [rows][groups * kSubs]
+    uint32_t* tops;        // [rows][groups]
+    double* sums;          // [rows][groups]
+    int32_t* flat;         // [rows]: 1: left to pass 3
+    int32_t groups;        // of the row that has most: its first vector may begin before it
+};
+
+// A row as 16-byte vectors: its elements stand `shift` places behind the vector grid's origin.
+template <typename T> struct Grid {
+    const T* origin;       // 16-byte aligned, at most 15 bytes before the row
+    int32_t shift;
+    int64_t vocab;
+    __device__ __forceinline__ Grid(const SampleArgs& a, int64_t row) : vocab(a.vocab) {
+        const uintptr_t p = (uintptr_t)((const T*)a.logits + row * a.row_stride);
+        shift = (int32_t)((p & 15) / sizeof(T));
+        origin = (const T*)(p & ~(uintptr_t)15);
+    }
+    __device__ __forceinline__ int32_t groups() const { return (int32_t)((vocab + shift + kGroup - 1) / kGroup); }
+    __device__ __forceinline__ bool has(int64_t at) const { return at >= shift && at < vocab + shift; }
+    __device__ __forceinline__ float operator()(int64_t at) const { return (float)origin[at]; }
+};
+
+// The 16 / sizeof(T) logits of the vector that begins at grid place `at`; places outside the row -inf.
+template <typename T>
+__device__ __forceinline__ void unpack(u32x4 raw, float* x) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(raw[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            x[e] = (float)__builtin_bit_cast(T, (unsigned short)(raw[e / 2] >> (16 * (e % 2))));
+    }
+}
+template <typename T>
+__device__ __forceinline__ u32x4 load_vector(const Grid<T>& z, int64_t at) {
+    return at < z.vocab + z.shift ? *(const u32x4*)(z.origin + at) : u32x4{0, 0, 0, 0};
+}
+
+template <int kCtrl>
+__device__ __forceinline__ float dpp_max(float x) {
+    const int y = __builtin_amdgcn_update_dpp(0, __float_as_int(x), kCtrl, 0xf, 0xf, true);
+    return fmaxf(x, __int_as_float(y));
+}
+template <int kCtrl>
+__device__ __forceinline__ double dpp_add(double x) {
+    const u32x2 u = __builtin_bit_cast(u32x2, x);
+    const u32x2 y = {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)u.x, kCtrl, 0xf, 0xf, true),
+                     (uint32_t)__builtin_amdgcn_update_dpp(0, (int)u.y, kCtrl, 0xf, 0xf, true)};
+    return x + __builtin_bit_cast(double, y);
+}
+constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kHalfMirror = 0x141, kMirror = 0x140;
+
+__device__ __forceinline__ float across_rows_max(float x) {
+    u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r.x), __uint_as_float(r.y));
+}
+// The sum over the wavefront, in every lane, in one order.
+__device__ __forceinline__ double wave_sum(double x) {
+    x = dpp_add<kXor1>(x);
+    x = dpp_add<kXor2>(x);
+    x = dpp_add<kHalfMirror>(x);
+    x = dpp_add<kMirror>(x);
+    u32x2 u = __builtin_bit_cast(u32x2, x);
+    u32x2 a = __builtin_amdgcn_permlane16_swap(u.x, u.x, false, false);
+    u32x2 b = __builtin_amdgcn_permlane16_swap(u.y, u.y, false, false);
+    x = __builtin_bit_cast(double, u32x2{a.x, b.x}) + __builtin_bit_cast(double, u32x2{a.y, b.y});
+    u = __builtin_bit_cast(u32x2, x);
+    a = __builtin_amdgcn_permlane32_swap(u.x, u.x, false, false);
+    b = __builtin_amdgcn_permlane32_swap(u.y, u.y, false, false);
+    return __builtin_bit_cast(double, u32x2{a.x, b.x}) + __builtin_bit_cast(double, u32x2{a.y, b.y});
+}
+
+// ------------------------------------------------------------ pass 1
+
+constexpr int kScanThreads = 256, kScanWaves = kScanThreads / 64;
+
+template <int kType>
+__global__ __launch_bounds__(kScanThreads) void asd_sample_scan_kernel(SampleArgs a, Stats s, int32_t per_wave,
+                                                                       int32_t tiles) {
+    typedef typename Element<kType>::T T;
+    constexpr int kPer = 16 / sizeof(T), kLoads = kGroup / (64 * kPer);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = blockIdx.x / tiles;
+    const int32_t tile = (int32_t)(blockIdx.x - row * tiles);
+    const Grid<T> z(a, row);
+    const Row r(a, row);
+    const bool whole = !r.greedy && !r.by_count;
+    const double per = 1.44269504088896340736 / (double)r.t;
+    // neighbouring wavefronts read neighbouring groups
+    const int32_t groups = z.groups();
+    int32_t g = (tile * per_wave) * kScanWaves + wave;
+    const int32_t stop = min((tile + 1) * per_wave * kScanWaves, s.groups);
+    u32x4 next[kLoads];
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) next[l] = load_vector(z, (int64_t)g * kGroup + (l * 64 + lane) * kPer);
+    for (; g < stop; g += kScanWaves) {
+        u32x4 raw[kLoads];
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            raw[l] = next[l];
+            next[l] = load_vector(z, (int64_t)(g + kScanWaves) * kGroup + (l * 64 + lane) * kPer);
+        }
+        const int64_t base = (int64_t)g * kGroup;
+        const bool inside = g > 0 && g + 1 < groups;         // every place is in the row
+        float top = -INFINITY;
+        bool any_nan = false;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            float x[kPer];
+            unpack<T>(raw[l], x);
+            float m = -INFINITY;
+            bool nan = false;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const float v = inside || z.has(base + (l * 64 + lane) * kPer + e) ? x[e] : -INFINITY;
+                nan |= v != v;
+                m = fmaxf(m, v);
+            }
+            m = dpp_max<kXor1>(m);
+            m = dpp_max<kXor2>(m);
+            m = dpp_max<kHalfMirror>(m);
+            if constexpr (kPer == 4) m = dpp_max<kMirror>(m);
+            top = fmaxf(top, m);
+            const u64 nans = __ballot(nan);
+            any_nan |= nans != 0;
+            constexpr int kLanes = kSub / kPer;              // of a sub-block
+            if (lane % kLanes == 0) {
+                const bool mine = (nans >> lane & ((1ull << kLanes) - 1)) != 0;
+                s.subs[(row * s.groups + g) * kSubs + l * (64 / kLanes) + lane / kLanes] = mine ? kKeyNan : key_of(m);
+            }
+        }
+        if constexpr (kPer == 8) top = dpp_max<kMirror>(top);
+        top = across_rows_max(top);
+        double sum = 0.0;
+        if (whole) {
+            const double from = top == -INFINITY ? 0.0 : (double)top;
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) {
+                float x[kPer];
+                unpack<T>(raw[l], x);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    const bool in = inside || z.has(base + (l * 64 + lane) * kPer + e);
+                    const double w = power2(((double)x[e] - from) * per);
+                    sum += !in || x[e] == -INFINITY ? 0.0 : x[e] == top ? 1.0 : top == INFINITY ? 0.0 : w;
+                }
+            }
+            sum = wave_sum(sum);
+        }
+        if (lane == 0) {
+            s.tops[row * s.groups + g] = any_nan ? kKeyNan : key_of(top);
+            s.sums[row * s.groups + g] = sum;
+        }
+    }
+}
+
+// ------------------------------------------------------------ workgroup sums
+
+template <int kN> struct Block {
+    static constexpr int kWaves = kN / 64;
+    double d[kWaves];
+    u64 u[kWaves];
+
+    __device__ __forceinline__ uint32_t max(uint32_t v) {
+        for (int x = 32; x > 0; x >>= 1) v = ::max(v, (uint32_t)__shfl_xor((int)v, x));
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) u[threadIdx.x >> 6] = v;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) v = ::max(v, (uint32_t)u[w]);
+        return v;
+    }
+    __device__ __forceinline__ uint32_t min(uint32_t v) { return ~max(~v); }
+    __device__ __forceinline__ uint32_t count(uint32_t v) {
+        for (int x = 32; x > 0; x >>= 1) v += (uint32_t)__shfl_xor((int)v, x);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) u[threadIdx.x >> 6] = v;
+        __syncthreads();
+        uint32_t sum = 0;
+        for (int w = 0; w < kWaves; ++w) sum += (uint32_t)u[w];
+        return sum;
+    }
+    __device__ __forceinline__ double sum(double v) {
+        v = wave_sum(v);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) d[threadIdx.x >> 6] = v;
+        __syncthreads();
+        double all = 0.0;
+        for (int w = 0; w < kWaves; ++w) all += d[w];
+        return all;
+    }
+    __device__ __forceinline__ u64 sum(u64 v) {
+        for (int x = 32; x > 0; x >>= 1) v += (u64)__shfl_xor((long long)v, x);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) u[threadIdx.x >> 6] = v;
+        __syncthreads();
+        u64 all = 0;
+        for (int w = 0; w < kWaves; ++w) all += u[w];
+        return all;
+    }
+    // sum over the threads before this one, and over all
+    template <typename V>
+    __device__ __forceinline__ V before(V v, V* box, V* total) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        V run = v;
+        for (int x = 1; x < 64; x <<= 1) {
+            const V up = __shfl_up(run, x);
+            if (lane >= x) run += up;
+        }
+        __syncthreads();
+        if (lane == 63) box[wave] = run;
+        __syncthreads();
+        V mine = 0, all = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) mine += box[w];
+            all += box[w];
+        }
+        *total = all;
+        return mine + (run - v);
+    }
+};
+
+// The first of wavefront 0's elements at which the running sum from `run` on passes `target`, lane
+// after lane, 16 to a lane from grid place `base`; the last one with a weight where rounding
+// leaves none.  Returns the grid place (every lane), and its weight.
+template <typename W>
+__device__ __forceinline__ int64_t draw_in_group(int64_t base, W&& weight, double run, double target, double* w) {
+    const int lane = threadIdx.x & 63;
+    double mine = 0.0;
+#pragma unroll 4
+    for (int e = 0; e < 16; ++e) mine += weight(base + lane * 16 + e);
+    double upto = mine;
+    for (int x = 1; x < 64; x <<= 1) {
+        const double up = __shfl_up(upto, x);
+        if (lane >= x) upto += up;
+    }
+    const u64 passes = __ballot(run + upto > target), some = __ballot(mine > 0.0);
+    const int at = passes ? __builtin_ctzll(passes) : 63 - __builtin_clzll(some);
+    int64_t place = -1;
+    double last = 0.0;
+    if (lane == at) {
+        double sum = run + (upto - mine);
+        for (int e = 0; e < 16; ++e) {
+            const double x = weight(base + lane * 16 + e);
+            sum += x;
+            if (x > 0.0) {
+                place = base + lane * 16 + e;
+                last = x;
+                if (sum > target) break;
+            }
+        }
+    }
+    *w = __shfl(last, at);
+    return __shfl((long long)place, at);
+}
+
+__device__ __forceinline__ float inside_unit(float u) {
+    return u >= 1.0f ? 0x1.fffffep-1f : u > 0.0f ? u : 0.0f;
+}
+
+// ------------------------------------------------------------ pass 2
+
+constexpr int kPickThreads = 256, kListed = 2048, kHeld = 16;
+constexpr int kMostSubs = kPickThreads * kHeld;          // sub-block maxima held in registers
+constexpr int kFewest = 512;                             // sub-blocks that candidates come from without top-k
+// Tokens that top-k may ask for here: as many sub-block maxima have to reach the threshold, which the
+// candidates then exceed by -ln(1 - k / subs) / (k / subs), 2.0 at 0.8, where the row is in no order.
+__device__ __forceinline__ int32_t most_k(int32_t subs) { return min(subs * 4 / 5, 1200); }
+
+template <int kType>
+__global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArgs a, Stats s) {
+    typedef typename Element<kType>::T T;
+    constexpr int kPer = 16 / sizeof(T);
+    __shared__ Block<kPickThreads> block;
+    __shared__ uint32_t key[kListed], place[kListed];
+    __shared__ double weight[kListed];
+    __shared__ int32_t wanted[kMostSubs / 2];
+    __shared__ int32_t found;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x;
+    const Grid<T> z(a, row);
+    const Row r(a, row);
+    const int32_t groups = z.groups(), subs = groups * kSubs;
+    const uint32_t* const sub = s.subs + row * s.groups * kSubs;
+    const uint32_t* const tops = s.tops + row * s.groups;
+    const double* const sums = s.sums + row * s.groups;
+    const auto finish = [&](int64_t at, double prob) {
+        a.out_token[row] = at < 0 ? -1 : (int32_t)(at - z.shift);
+        if (a.out_prob) a.out_prob[row] = (float)prob;
+    };
+    if (tid == 0) s.flat[row] = 0;
+
+    uint32_t top = 0;
+    for (int32_t g = tid; g < groups; g += kPickThreads) top = max(top, tops[g]);
+    top = block.max(top);
+    if (top == kKeyNan || top == kKeyNegInf) {
+        if (tid == 0) {
+            finish(-1, 0.0);
+            atomicOr(a.error_word, kDecodeErrSample);
+        }
+        return;
+    }
+    if (r.greedy) {
+        uint32_t first = ~0u;
+        for (int32_t g = tid; g < groups && first == ~0u; g += kPickThreads)
+            if (tops[g] == top) first = (uint32_t)g;
+        first = block.min(first);
+        if (wave == 0) {
+            const uint32_t k = lane < kSubs ? sub[(int64_t)first * kSubs + lane] : 0;
+            const int64_t at = (int64_t)first * kGroup + __builtin_ctzll(__ballot(k == top)) * kSub + lane;
+            const u64 same = __ballot(z.has(at) && key_of(z(min(max(at, (int64_t)z.shift), z.vocab + z.shift - 1))) == top);
+            if (lane == 0) finish(at + __builtin_ctzll(same), 1.0);
+        }
+        return;
+    }
+    const Weights w(value_of(top), r.t);
+    const float u = inside_unit(a.uniform[row]);
+
+    double all = 0.0;           // the row's weights, where they count
+    const bool filtered = r.by_count || r.by_mass || r.by_floor;
+    if (!r.by_count) {
+        if (!filtered) {
+            // the draw's group
+            const int32_t each = (groups + kPickThreads - 1) / kPickThreads;
+            const int32_t from = min(groups, tid * each), to = min(groups, from + each);
+            double mine = 0.0;
+            for (int32_t g = from; g < to; ++g) mine += sums[g] * w(value_of(tops[g]));
+            const double before = block.before(mine, block.d, &all), target = (double)u * all;
+            // the first thread whose share passes it; rounding may leave none: the last with a weight
+            uint32_t passes = mine > 0.0 && before + mine > target ? (uint32_t)tid : ~0u;
+            passes = block.min(passes);
+            if (passes == ~0u) passes = block.max(mine > 0.0 ? (uint32_t)tid : 0u);
+            if ((uint32_t)tid == passes) {
+                double run = before;
+                for (int32_t g = from; g < to; ++g) {
+                    const double x = sums[g] * w(value_of(tops[g]));
+                    if (x > 0.0) {
+                        found = g;
+                        weight[0] = run;        // of the tokens before the group
+                    }
+                    if (run + x > target) break;
+                    run += x;
+                }
+            }
+            __syncthreads();
+            if (wave == 0) {
+                double x;
+                const int64_t at = draw_in_group(
+                    (int64_t)found * kGroup,
+                    [&](int64_t place) { return z.has(place) ? w(z(place)) : 0.0; }, weight[0], target, &x);
+                if (lane == 0) finish(at, x / all);
+            }
+            return;
+        }
+        double mine = 0.0;
+        for (int32_t g = tid; g < groups; g += kPickThreads) mine += sums[g] * w(value_of(tops[g]));
+        all = block.sum(mine);
+    }
+
+    // Candidates: every token whose key reaches `least`, which `need` sub-blocks' maxima do.
+    const int32_t need = r.by_count ? r.k : max(1, min(kFewest, subs / 2));
+    if (subs > kMostSubs || (r.by_count && r.k > most_k(subs))) {
+        if (tid == 0) s.flat[row] = 1;
+        return;
+    }
+    uint32_t held[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = i * kPickThreads + tid < subs ? sub[i * kPickThreads + tid] : 0;
+    uint32_t least = 0;         // by bisection over its upper 16 bits
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t trial = least | 1u << bit;
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) n += held[i] >= trial;
+        if (block.count(n) >= (uint32_t)need) least = trial;
+    }
+    least = max(least, kKeyNegInf);
+    // the sub-blocks that reach it, in order
+    int32_t blocks = 0;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        if (i * kPickThreads >= subs) break;
+        const bool in = held[i] >= least;
+        int32_t total;
+        const int32_t at = blocks + block.before((int32_t)in, (int32_t*)block.u, &total);
+        if (in && at < kMostSubs / 2) wanted[at] = i * kPickThreads + tid;
+        blocks += total;
+    }
+    __syncthreads();
+    // their tokens, in order
+    int32_t n = 0;
+    constexpr int kLanes = kSub / kPer, kAtOnce = kPickThreads / kLanes;
+    if (blocks <= kMostSubs / 2) {
+        for (int32_t b = 0; b < blocks && n <= kListed; b += kAtOnce) {
+            const int32_t i = b + tid / kLanes;
+            int64_t at = 0;
+            uint32_t k[kPer];
+            int32_t mine = 0;
+            if (i < blocks) {
+                at = (int64_t)wanted[i] * kSub + tid % kLanes * kPer;
+                float x[kPer];
+                unpack<T>(load_vector(z, at), x);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    k[e] = z.has(at + e) ? key_of(x[e]) : 0;
+                    mine += k[e] >= least;
+                }
+            }
+            int32_t total;
+            int32_t to = n + block.before(mine, (int32_t*)block.u, &total);
+            if (i < blocks) {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if (k[e] >= least) {
+                        if (to < kListed) {
+                            key[to] = k[e];
+                            place[to] = (uint32_t)(at + e);
+                        }
+                        ++to;
+                    }
+            }
+            n += total;
+        }
+    }
+    if (blocks > kMostSubs / 2 || n > kListed) {
+        if (tid == 0) s.flat[row] = 1;
+        return;
+    }
+    __syncthreads();
+    double sum = 0.0;
+    for (int i = tid; i < n; i += kPickThreads) sum += weight[i] = w(value_of(key[i]));
+    // (every thread keeps to the candidates tid, tid + 256, ...; sums over them are the block's, in one order)
+
+    // The greatest key that enough tokens, or tokens of enough weight, reach; the first `ties` of
+    // those that have it are kept.
+    uint32_t cut = 0;
+    int32_t ties = 0x7fffffff;
+    if (r.by_count) {
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t trial = cut | 1u << bit;
+            uint32_t c = 0;
+            for (int i = tid; i < n; i += kPickThreads) c += key[i] >= trial;
+            if (block.count(c) >= (uint32_t)r.k) cut = trial;
+        }
+        uint32_t c = 0;
+        double mine = 0.0;
+        for (int i = tid; i < n; i += kPickThreads)
+            if (key[i] > cut) {
+                ++c;
+                mine += weight[i];
+            }
+        ties = r.k - (int32_t)block.count(c);
+        all = block.sum(mine) + ties * w(value_of(cut));
+    } else {
+        sum = block.sum(sum);
+        const bool everything = least == kKeyNegInf;        // no token is left out
+        if (!everything && !(r.by_mass && sum >= (double)r.p * all) &&
+            !(r.by_floor && w(value_of(least)) < (double)r.m)) {
+            if (tid == 0) s.flat[row] = 1;
+            return;
+        }
+        // (where the floor alone bounds the candidates, the nucleus may be larger than they are: all of them)
+        if (!everything && r.by_mass && sum < (double)r.p * all) cut = least;
+    }
+    if (r.by_mass && (r.by_count || cut == 0)) {
+        const double goal = (double)r.p * all;
+        const uint32_t limit = cut;
+        const int32_t limit_ties = ties;
+        // tokens at `limit` beyond its ties do not count
+        uint32_t same = 0;
+        if (r.by_count) {
+            uint32_t c = 0;
+            for (int i = tid; i < n; i += kPickThreads) c += key[i] == limit;
+            same = block.count(c);
+        }
+        const double beyond = r.by_count ? ((int32_t)same - limit_ties) * w(value_of(limit)) : 0.0;
+        uint32_t t = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t trial = t | 1u << bit;
+            double mine = 0.0;
+            for (int i = tid; i < n; i += kPickThreads)
+                if (key[i] >= trial) mine += weight[i];
+            const double reach = block.sum(mine) - (trial <= limit ? beyond : 0.0);
+            if (reach >= goal && reach > 0.0) t = trial;
+        }
+        if (t > limit || !r.by_count) {
+            double mine = 0.0;
+            for (int i = tid; i < n; i += kPickThreads)
+                if (key[i] > t) mine += weight[i];
+            const double above = block.sum(mine), one = w(value_of(t));
+            cut = t;
+            ties = max(1, one > 0.0 ? (int32_t)min(ceil((goal - above) / one), 2e9) : 1);
+        } else {
+            double mine = 0.0;
+            for (int i = tid; i < n; i += kPickThreads)
+                if (key[i] > limit) mine += weight[i];
+            const double above = block.sum(mine), one = w(value_of(limit));
+            ties = min(limit_ties, max(1, one > 0.0 ? (int32_t)min(ceil((goal - above) / one), 2e9) : 1));
+        }
+    }
+
+    // What is kept, in order, and the draw.  (A thread takes neighbouring candidates.)
+    const double floor = r.by_floor ? (double)r.m : 0.0;
+    const int each = (n + kPickThreads - 1) / kPickThreads, from = min(n, tid * each), to = min(n, from + each);
+    int32_t at_cut = 0, total_cut;
+    for (int i = from; i < to; ++i) at_cut += key[i] == cut;
+    at_cut = block.before(at_cut, (int32_t*)block.u, &total_cut);
+    const auto kept = [&](int i, int32_t& seen) {
+        if (key[i] < cut || (key[i] == cut && seen++ >= ties)) return 0.0;
+        return weight[i] >= floor ? weight[i] : 0.0;
+    };
+    int32_t seen = at_cut;
+    double mine = 0.0, total;
+    for (int i = from; i < to; ++i) mine += kept(i, seen);
+    const double before = block.before(mine, block.d, &total), target = (double)u * total;
+    uint32_t passes = block.min(mine > 0.0 && before + mine > target ? (uint32_t)tid : ~0u);
+    if (passes == ~0u) passes = block.max(mine > 0.0 ? (uint32_t)tid : 0u);
+    if ((uint32_t)tid == passes) {
+        seen = at_cut;
+        double run = before, x = 0.0;
+        int at = from;
+        for (int i = from; i < to; ++i) {
+            const double y = kept(i, seen);
+            run += y;
+            if (y > 0.0) {
+                at = i;
+                x = y;
+                if (run > target) break;
+            }
+        }
+        finish((int64_t)place[at], x / total);
+    }
+}
+
+// ------------------------------------------------------------ pass 3
+
+constexpr int kFlatThreads = 1024, kFlatWaves = kFlatThreads / 64, kBins = 4096, kCollected = 8192, kSpans = 1024;
+
+// ceil and floor of f * total for a float 0 <= f < 1 and an integer below 2^63, exactly.
+__device__ __forceinline__ u64 share(float f, u64 total, bool up) {
     if (!(f > 0.0f)) return 0;
     int e;
     const uint32_t m = (uint32_t)ldexpf(frexpf(f, &e), 24);   // f = m 2^(e - 24)
     const int shift = 24 - e;
     const unsigned __int128 x = (unsigned __int128)total * m;
-    if (shift >= 120) return x != 0;
-    return (u64)((x + (((unsigned __int128)1 << shift) - 1)) >> shift);
-}
-__device__ __forceinline__ u64 share_floor(float f, u64 total) {
-    if (!(f > 0.0f)) return 0;
-    int e;
-    const uint32_t m = (uint32_t)ldexpf(frexpf(f, &e), 24);
-    const int shift = 24 - e;
-    if (shift >= 120) return 0;
-    return (u64)(((unsigned __int128)total * m) >> shift);
+    if (shift >= 120) return up && x != 0;
+    return (u64)((x + (up ? ((unsigned __int128)1 << shift) - 1 : 0)) >> shift);
 }
 
-// One workgroup per row, which it reads several times: the greatest logit, the
-// ranking's cut by two radix selections (by count, by weight), the kept
-// weights of 1,024 stretches of the row, and the stretch the draw falls in.
+// A workgroup a row.  Weights are whole numbers of 2^-bits of the greatest, so that sums over any order are
+// the same; spans of `span` tokens (1,024 up to 2^20 tokens a row) hold what is kept of them.
 template <int kType>
-__global__ __launch_bounds__(kThreads) void asd_sample_kernel(SampleArgs a, int bits) {
+__global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArgs a, Stats s, int bits) {
     typedef typename Element<kType>::T T;
-    __shared__ u64 box[kWaves];
-    __shared__ u64 weight_bin[256];
-    __shared__ unsigned count_bin[256];
-    __shared__ u64 part[kThreads];
-    __shared__ unsigned ties[kThreads];
+    constexpr int kPer = 16 / sizeof(T);
+    __shared__ Block<kFlatThreads> block;
+    __shared__ u64 bin_weight[kBins];
+    __shared__ uint32_t bin_count[kBins];
+    __shared__ uint32_t key[kCollected];
+    __shared__ u64 span_sum[kSpans];
+    __shared__ uint32_t span_ties[kSpans];
+    __shared__ uint32_t collected;
     __shared__ u64 pick[4];
-    const int tid = threadIdx.x;
-    const int64_t row = blockIdx.x, vocab = a.vocab;
-    const T* z = (const T*)a.logits + row * a.row_stride;
-
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t row = blockIdx.x;
+    if (s.flat[row] == 0) return;
+    const Grid<T> z(a, row);
+    const Row r(a, row);
+    const int32_t groups = z.groups(), per_span = (groups + kSpans - 1) / kSpans;
+    const int32_t spans = (groups + per_span - 1) / per_span;
     uint32_t top = 0;
-    for (int64_t v = tid; v < vocab; v += kThreads) {
-        const uint32_t k = key_of((float)z[v]);
-        top = k > top ? k : top;
-    }
-    top = (uint32_t)block_reduce<u64>(top, [](u64 x, u64 y) { return x > y ? x : y; }, box);
-    if (top == kKeyNan || top == kKeyNegInf) {
-        if (tid == 0) {
-            a.out_token[row] = -1;
-            if (a.out_prob) a.out_prob[row] = 0.0f;
-            atomicOr(a.error_word, kDecodeErrSample);
-        }
-        return;
-    }
-    const float t = a.temperature ? a.temperature[row] : 1.0f;
-    if (!(t > 0.0f)) {
-        u64 first = ~0ull;
-        for (int64_t v = tid; v < vocab; v += kThreads)
-            if (key_of((float)z[v]) == top) {
-                first = (u64)v;
-                break;
-            }
-        first = block_reduce<u64>(first, [](u64 x, u64 y) { return x < y ? x : y; }, box);
-        if (tid == 0) {
-            a.out_token[row] = (int32_t)first;
-            if (a.out_prob) a.out_prob[row] = 1.0f;
-        }
-        return;
-    }
-    Weights w;
-    w.top_f = value_of(top);
-    w.top = (double)w.top_f;
-    w.per = 1.44269504088896340736 / (double)t;
-    w.unit = (double)(1ull << bits);
+    for (int32_t g = tid; g < groups; g += kFlatThreads) top = max(top, s.tops[row * s.groups + g]);
+    top = block.max(top);
+    const Weights w(value_of(top), r.t);
+    const double unit = (double)(1ull << bits), least = r.by_floor ? (double)r.m : 0.0;
+    const auto fixed = [&](double x) { return (u64)(x * unit + 0.5); };
 
-    // The kept prefix: keys above `cut`, and the first `cut_ties` tokens whose key is `cut`.
-    const int32_t k = a.top_k ? a.top_k[row] : 0;
-    const float p = a.top_p ? a.top_p[row] : 1.0f;
-    const bool by_count = k > 0 && k < vocab, by_mass = p < 1.0f;
-    uint32_t cut = 0;
-    u64 cut_ties = ~0ull;
-    const auto add = [](u64 x, u64 y) { return x + y; };
-    for (int stage = 0; stage < 2; ++stage) {
-        if (!(stage == 0 ? by_count : by_mass)) continue;
-        // what the keys of earlier stages leave: stage 1 counts keys above `limit` whole and
-        // `limit_ties` tokens at it
-        const uint32_t limit = cut;
-        const u64 limit_ties = cut_ties;
-        u64 want = (u64)k;
-        if (stage == 1) {
-            u64 sum = 0, at = 0;
-            for (int64_t v = tid; v < vocab; v += kThreads) {
-                const float x = (float)z[v];
-                const uint32_t key = key_of(x);
-                if (key > limit) sum += w.fixed(w.real(x));
-                at += key == limit;
+    // Calls f(key, value, grid place) for every token of the row, group by group, a wavefront each; a group's
+    // end is told by end(group).
+    const auto over = [&](auto&& f, auto&& end) {
+        constexpr int kLoads = kGroup / (64 * kPer);
+        u32x4 next[kLoads];
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) next[l] = load_vector(z, (int64_t)wave * kGroup + (l * 64 + lane) * kPer);
+        for (int32_t g = wave; g < groups; g += kFlatWaves) {
+            u32x4 raw[kLoads];
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) {
+                raw[l] = next[l];
+                next[l] = load_vector(z, (int64_t)(g + kFlatWaves) * kGroup + (l * 64 + lane) * kPer);
             }
-            sum = block_reduce<u64>(sum, add, box);
-            at = block_reduce<u64>(at, add, box);
-            at = at < limit_ties ? at : limit_ties;
-            sum += at * w.fixed(w.real(value_of(limit)));
-            want = share_ceil(p, sum);
-            if (want < 1) want = 1;
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) {
+                float x[kPer];
+                unpack<T>(raw[l], x);
+                const int64_t at = (int64_t)g * kGroup + (l * 64 + lane) * kPer;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if (z.has(at + e)) f(key_of(x[e]), x[e], at + e);
+            }
+            end(g);
         }
-        uint32_t prefix = 0;
-        for (int level = 3; level >= 0; --level) {
-            for (int b = tid; b < 256; b += kThreads) weight_bin[b] = count_bin[b] = 0;
-            __syncthreads();
-            const uint32_t above = level == 3 ? 0u : ~0u << (8 * level + 8);
-            for (int64_t v = tid; v < vocab; v += kThreads) {
-                const float x = (float)z[v];
-                const uint32_t key = key_of(x);
-                if ((key & above) != prefix || key < limit) continue;
-                const int b = (key >> (8 * level)) & 255;
-                if (stage == 1 && key > limit) atomicAdd(&weight_bin[b], w.fixed(w.real(x)));
-                if (stage == 0 || key == limit) atomicAdd(&count_bin[b], 1u);
+    };
+    const auto nothing = [](int32_t) {};
+
+    // Keys above `cut` are kept, and the first `ties` tokens that have it; stage 0 cuts by count, stage 1 by
+    // mass among what stage 0 left.
+    uint32_t cut = 0;
+    u64 ties = ~0ull;
+    for (int stage = 0; stage < 2; ++stage) {
+        if (!(stage == 0 ? r.by_count : r.by_mass)) continue;
+        const uint32_t limit = cut;
+        const u64 limit_ties = ties, limit_weight = limit ? fixed(w(value_of(limit))) : 0;
+        u64 want = (u64)r.k;
+        uint32_t prefix = 0;            // of the cut's key, from bit `shift` up
+        int shift = 32;
+        u64 in_bin = 0;
+        while (shift > 0) {
+            const int low = shift == 32 ? 20 : shift == 20 ? 8 : 0;
+            const uint32_t mask = (1u << (shift - low)) - 1;
+            for (int b = tid; b < kBins; b += kFlatThreads) {
+                bin_weight[b] = 0;
+                bin_count[b] = 0;
             }
             __syncthreads();
-            if (tid == 0) {
-                // the bin in which the wanted amount is reached, from the greatest key down
-                u64 have = 0;
-                int b = 255;
-                const u64 limit_weight = stage == 1 ? w.fixed(w.real(value_of(limit))) : 0;
-                for (; b > 0; --b) {
-                    u64 here = count_bin[b];
-                    if (stage == 1) {
-                        here = here < limit_ties ? here : limit_ties;
-                        here = weight_bin[b] + here * limit_weight;
+            over(
+                [&](uint32_t k, float x, int64_t) {
+                    if (k < limit || (shift < 32 && k >> shift != prefix)) return;
+                    const uint32_t b = k >> low & mask;
+                    if (stage == 1 && k > limit) atomicAdd(&bin_weight[b], fixed(w(x)));
+                    atomicAdd(&bin_count[b], 1u);
+                },
+                nothing);
+            __syncthreads();
+            // of the tokens at the limit only those count that stage 0 kept
+            if (stage == 1 && limit != 0 && (shift == 32 || limit >> shift == prefix) && tid == 0)
+                bin_weight[limit >> low & mask] += limit_ties * limit_weight;
+            __syncthreads();
+            if (stage == 1 && shift == 32) {
+                u64 mine = 0;
+                for (int b = tid; b < kBins; b += kFlatThreads) mine += bin_weight[b];
+                want = max((u64)1, share(r.p, block.sum(mine), true));
+            }
+            // the bin in which the wanted amount is reached, from the greatest key down: four bins a thread
+            u64 four[4], mine = 0, total;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int b = kBins - 1 - (4 * tid + i);
+                four[i] = stage == 1 ? bin_weight[b] : bin_count[b];
+                mine += four[i];
+            }
+            u64 have = block.before(mine, block.u, &total);
+            if (tid == 0) {         // none: the last token there is
+                pick[0] = 0;
+                pick[1] = want;
+            }
+            __syncthreads();
+            if (have < want && have + mine >= want) {
+                for (int i = 0; i < 4; ++i) {
+                    if (have + four[i] >= want) {
+                        pick[0] = (u64)(kBins - 1 - (4 * tid + i));
+                        pick[1] = want - have;
+                        break;
                     }
-                    if (have + here >= want) break;
-                    have += here;
+                    have += four[i];
                 }
-                pick[0] = (u64)b;
-                pick[1] = want - have;
             }
             __syncthreads();
-            prefix |= (uint32_t)pick[0] << (8 * level);
+            prefix = (shift == 32 ? 0u : prefix << (shift - low)) | (uint32_t)pick[0];
             want = pick[1];
+            in_bin = bin_count[pick[0]];
+            shift = low;
             __syncthreads();
+            if (in_bin <= (u64)kCollected) break;
+        }
+        if (shift > 0) {
+            // the bin's tokens, and the cut among them
+            if (tid == 0) collected = 0;
+            __syncthreads();
+            over(
+                [&](uint32_t k, float, int64_t at) {
+                    if (k >= limit && k >> shift == prefix) {
+                        const uint32_t i = atomicAdd(&collected, 1u);
+                        if (i < kCollected) key[i] = k;
+                    }
+                },
+                nothing);
+            __syncthreads();
+            const int n = min((int)collected, kCollected);
+            const bool limit_in = stage == 1 && limit != 0 && limit >> shift == prefix;
+            for (int bit = shift - 1; bit >= 0; --bit) {
+                const uint32_t trial = (prefix << (shift - bit) | 1u) << bit;
+                u64 mine = 0;
+                for (int i = tid; i < n; i += kFlatThreads) {
+                    if (key[i] < trial) continue;
+                    mine += stage == 0 ? 1 : key[i] > limit ? fixed(w(value_of(key[i]))) : 0;
+                }
+                u64 reach = block.sum(mine);
+                if (limit_in && trial <= limit) reach += limit_ties * limit_weight;
+                prefix = prefix << 1 | (reach >= want ? 1u : 0u);
+                shift = bit;
+            }
+            u64 mine = 0;
+            for (int i = tid; i < n; i += kFlatThreads)
+                if (key[i] > prefix) mine += stage == 0 ? 1 : key[i] > limit ? fixed(w(value_of(key[i]))) : 0;
+            want -= min(want, block.sum(mine));
         }
         cut = prefix;
         if (stage == 0) {
-            cut_ties = want;
+            ties = want;
         } else {
-            const u64 one = w.fixed(w.real(value_of(cut)));
-            u64 n = one > 0 ? (want + one - 1) / one : 1;
-            if (n < 1) n = 1;
-            cut_ties = cut == limit && n > limit_ties ? limit_ties : n;
+            const u64 one = fixed(w(value_of(cut)));
+            const u64 m = max((u64)1, one > 0 ? (want + one - 1) / one : 1);
+            ties = cut == limit ? min(m, limit_ties) : m;
         }
     }
-    const float m = a.min_p ? a.min_p[row] : 0.0f;
-    const double least = m > 0.0f ? (m < 1.0f ? (double)m : 1.0) : 0.0;
 
-    // The kept weight of every thread's stretch, ties at the cut in index order.
-    const int64_t stretch = (vocab + kThreads - 1) / kThreads;
-    const int64_t from = tid * stretch < vocab ? tid * stretch : vocab;
-    const int64_t to = from + stretch < vocab ? from + stretch : vocab;
-    unsigned n = 0;
-    for (int64_t v = from; v < to; ++v) n += key_of((float)z[v]) == cut;
-    ties[tid] = n;
+    // What every span keeps: the weights above the cut, and how many tokens have its key.
+    for (int i = tid; i < kSpans; i += kFlatThreads) {
+        span_sum[i] = 0;
+        span_ties[i] = 0;
+    }
     __syncthreads();
-    if (tid == 0) {
-        unsigned sum = 0;
-        for (int j = 0; j < kThreads; ++j) {
-            const unsigned c = ties[j];
-            ties[j] = sum;
-            sum += c;
+    u64 mine = 0;
+    uint32_t same = 0;
+    over(
+        [&](uint32_t k, float x, int64_t) {
+            if (k > cut) {
+                const double real = w(x);
+                mine += real >= least ? fixed(real) : 0;
+            }
+            same += k == cut;
+        },
+        [&](int32_t g) {
+            for (int x = 32; x > 0; x >>= 1) {
+                mine += (u64)__shfl_xor((long long)mine, x);
+                same += (uint32_t)__shfl_xor((int)same, x);
+            }
+            if (lane == 0) {
+                atomicAdd(&span_sum[g / per_span], mine);
+                atomicAdd(&span_ties[g / per_span], same);
+            }
+            mine = 0;
+            same = 0;
+        });
+    __syncthreads();
+    const double cut_real = w(value_of(cut));
+    const u64 cut_weight = cut_real >= least ? fixed(cut_real) : 0;
+    const u64 here = tid < spans ? span_ties[tid] : 0;
+    u64 total;
+    const u64 ties_before = block.before(here, block.u, &total);
+    const u64 kept_ties = ties_before < ties ? min(here, ties - ties_before) : 0;
+    const u64 sum = tid < spans ? span_sum[tid] + kept_ties * cut_weight : 0;
+    const u64 before = block.before(sum, block.u, &total);
+    const float u = inside_unit(a.uniform[row]);
+    if (u == 0.0f) {
+        // the first kept token, which may weigh less than a unit
+        uint32_t first = ~0u;
+        double weight = 0.0;
+        over(
+            [&](uint32_t k, float x, int64_t at) {
+                if (k < cut || first != ~0u) return;
+                const double real = w(x);
+                if (real > 0.0 && real >= least) {
+                    first = (uint32_t)at;
+                    weight = real;
+                }
+            },
+            nothing);
+        const uint32_t place = block.min(first);
+        if (first == place) {
+            a.out_token[row] = (int32_t)(place - (uint32_t)z.shift);
+            if (a.out_prob) a.out_prob[row] = (float)(weight * unit / (double)total);
         }
+        return;
     }
-    __syncthreads();
-    const auto kept = [&](float x, u64& seen) -> u64 {
-        const uint32_t key = key_of(x);
-        if (key < cut || (key == cut && seen++ >= cut_ties)) return 0;
-        const double real = w.real(x);
-        return real >= least ? w.fixed(real) : 0;
-    };
-    u64 seen = ties[tid], sum = 0;
-    for (int64_t v = from; v < to; ++v) sum += kept((float)z[v], seen);
-    part[tid] = sum;
-    __syncthreads();
-    if (tid == 0) {
-        u64 total = 0;
-        for (int j = 0; j < kThreads; ++j) total += part[j];
-        float u = a.uniform[row];
-        u = u < 0x1.fffffep-1f ? u : u >= 1.0f ? 0x1.fffffep-1f : u;
-        const u64 target = share_floor(u, total);      // the running sum has to exceed it
-        u64 before = 0;
-        int j = 0;
-        while (before + part[j] <= target) before += part[j++];
-        pick[0] = (u64)j;
+    const u64 target = share(u, total, false);     // the running sum has to exceed it
+    if (sum > 0 && before <= target && before + sum > target) {
+        pick[0] = (u64)tid;
         pick[1] = before;
-        pick[2] = target;
-        pick[3] = total;
+        pick[2] = ties_before;
     }
     __syncthreads();
-    if ((u64)tid == pick[0]) {
-        u64 run = pick[1];
-        seen = ties[tid];
-        for (int64_t v = from; v < to; ++v) {
-            const u64 x = kept((float)z[v], seen);
-            run += x;
-            if (run > pick[2]) {
-                a.out_token[row] = (int32_t)v;
-                if (a.out_prob) a.out_prob[row] = (float)((double)x / (double)pick[3]);
+    // the span's tokens in order, 64 at a time
+    if (wave == 0) {
+        u64 run = pick[1], seen = pick[2];
+        const int64_t from = (int64_t)pick[0] * per_span * kGroup, to = min(from + (int64_t)per_span * kGroup,
+                                                                          z.vocab + z.shift);
+        for (int64_t at = from; at < to; at += 64) {
+            const bool in = at + lane < to && z.has(at + lane);
+            const float x = in ? z(at + lane) : -INFINITY;
+            const uint32_t k = in ? key_of(x) : 0;
+            const u64 tied = __ballot(in && k == cut);
+            const u64 rank = seen + __popcll(tied & ((1ull << lane) - 1));
+            u64 y = 0;
+            if (in && (k > cut || (k == cut && rank < ties))) {
+                const double real = w(x);
+                y = real >= least ? fixed(real) : 0;
+            }
+            u64 upto = y;
+            for (int d = 1; d < 64; d <<= 1) {
+                const u64 up = (u64)__shfl_up((long long)upto, d);
+                if (lane >= d) upto += up;
+            }
+            const u64 passes = __ballot(run + upto > target);
+            if (passes) {
+                if (lane == __builtin_ctzll(passes)) {
+                    a.out_token[row] = (int32_t)(at + lane - z.shift);
+                    if (a.out_prob) a.out_prob[row] = (float)((double)y / (double)total);
+                }
                 break;
             }
+            run += (u64)__shfl((long long)upto, 63);
+            seen += __popcll(tied);
         }
     }
+}
+
+int32_t most_groups(int64_t vocab) { return (int32_t)((vocab + 7 + kGroup - 1) / kGroup); }
+
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+template <int kType>
+hipError_t sample(const SampleArgs& a, const Stats& s, int32_t per_wave, int bits, hipStream_t stream) {
+    const int32_t tiles = (s.groups + per_wave * kScanWaves - 1) / (per_wave * kScanWaves);
+    asd_sample_scan_kernel<kType><<<(unsigned)(a.rows * tiles), kScanThreads, 0, stream>>>(a, s, per_wave, tiles);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+    asd_sample_pick_kernel<kType><<<(unsigned)a.rows, kPickThreads, 0, stream>>>(a, s);
+    if ((err = hipGetLastError()) != hipSuccess) return err;
+    asd_sample_flat_kernel<kType><<<(unsigned)a.rows, kFlatThreads, 0, stream>>>(a, s, bits);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t sample_workspace_bytes(int64_t, int64_t, int) { return 0; }
+size_t sample_workspace_bytes(int64_t vocab, int64_t rows, int) {
+    const size_t groups = (size_t)most_groups(vocab) * (size_t)rows;
+    return align256(groups * sizeof(double)) + align256(groups * kSubs * 4) + align256(groups * 4) +
+           align256((size_t)rows * 4);
+}
 
-hipError_t launch_sample(const SampleArgs& a, asd_dtype dtype, void*, int, hipStream_t stream) {
+hipError_t launch_sample(const SampleArgs& a, asd_dtype dtype, void* workspace, int cus, hipStream_t stream) {
     int bits = 62;
     while (((int64_t)1 << (62 - bits)) < a.vocab) --bits;
     if (bits > 52) bits = 52;
-    const dim3 grid((unsigned)a.rows);
-    if (dtype == ASD_F32)
-        asd_sample_kernel<ASD_F32><<<grid, kThreads, 0, stream>>>(a, bits);
-    else if (dtype == ASD_BF16)
-        asd_sample_kernel<ASD_BF16><<<grid, kThreads, 0, stream>>>(a, bits);
-    else
-        asd_sample_kernel<ASD_F16><<<grid, kThreads, 0, stream>>>(a, bits);
-    return hipGetLastError();
+    Stats s;
+    s.groups = most_groups(a.vocab);
+    const size_t groups = (size_t)s.groups * (size_t)a.rows;
+    char* p = (char*)workspace;
+    s.sums = (double*)p;
+    p += align256(groups * sizeof(double));
+    s.subs = (uint32_t*)p;
+    p += align256(groups * kSubs * 4);
+    s.tops = (uint32_t*)p;
+    p += align256(groups * 4);
+    s.flat = (int32_t*)p;
+    // groups a wavefront takes: as many as leave eight workgroups to a compute unit, eight at most
+    int64_t per_wave = (int64_t)groups / ((int64_t)cus * 8 * kScanWaves);
+    per_wave = per_wave < 1 ? 1 : per_wave > 8 ? 8 : per_wave;
+    while (a.rows * ((s.groups + per_wave * kScanWaves - 1) / (per_wave * kScanWaves)) >= ((int64_t)1 << 31))
+        per_wave *= 2;
+    if (dtype == ASD_F32) return sample<ASD_F32>(a, s, (int32_t)per_wave, bits, stream);
+    if (dtype == ASD_BF16) return sample<ASD_BF16>(a, s, (int32_t)per_wave, bits, stream);
+    return sample<ASD_F16>(a, s, (int32_t)per_wave, bits, stream);
 }
 
 }  // namespace asd
