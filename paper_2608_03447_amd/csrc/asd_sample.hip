@@ -50,14 +50,16 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
-constexpr uint32_t kKeyNegInf = 0x007fffffu, kKeyNan = 0xffffffffu;
+constexpr uint32_t kKeyNegInf = 0x007fffffu, kKeyInf = 0xff800000u, kKeyNan = 0xffffffffu;
 
 // 2^x for x <= 0, to 2^-47: the Taylor polynomial of degree 11 of 2^r, |r| <= 1/2
-// (the next term is (ln 2 / 2)^12 / 12! = 6e-15).  2^0 is 1 exactly; below 2^-1000 it is 0.
-__device__ __forceinline__ double power2(double x) {
-    const bool none = x < -1000.0;
+// (the next term is (ln 2 / 2)^12 / 12! = 6e-15).  2^0 is 1 exactly; x below -1000 gives 2^-1000.
+// Adding 1.5 2^52 rounds x to a whole number, which stands in the sum's low bits and goes into
+// the result's exponent by one integer addition: conversions and ldexp run at a quarter of the rate.
+__device__ __forceinline__ double power2_clamped(double x) {
+    constexpr double kRound = 6755399441055744.0;
     x = fmax(x, -1000.0);
-    const double n = rint(x), r = x - n;
+    const double t = x + kRound, r = x - (t - kRound);
     double p = 4.4455382718708114e-10;                 // ln(2)^k / k!, k = 11 .. 1
     p = fma(p, r, 7.0549116208011232e-09);
     p = fma(p, r, 1.0178086009239700e-07);
@@ -70,7 +72,9 @@ __device__ __forceinline__ double power2(double x) {
     p = fma(p, r, 2.4022650695910071e-01);
     p = fma(p, r, 6.9314718055994531e-01);
     p = fma(p, r, 1.0);
-    return none ? 0.0 : ldexp(p, (int)n);
+    const u64 bits = __builtin_bit_cast(u64, p);
+    return __builtin_bit_cast(double, (u64)((uint32_t)(bits >> 32) + ((uint32_t)__builtin_bit_cast(u64, t) << 20)) << 32 |
+                                          (uint32_t)bits);
 }
 
 // A row's weights, exp((z - top) / T).
@@ -80,8 +84,8 @@ struct Weights {
     __device__ __forceinline__ Weights(float greatest, float t)
         : top((double)greatest), per(1.44269504088896340736 / (double)t), top_f(greatest) {}
     __device__ __forceinline__ double operator()(float z) const {
-        const double w = power2(((double)z - top) * per);
-        return z == top_f ? 1.0 : z == -INFINITY || top_f == INFINITY ? 0.0 : w;
+        const double x = ((double)z - top) * per, w = power2_clamped(x);
+        return z == top_f ? 1.0 : !(x >= -1000.0) || z == -INFINITY || top_f == INFINITY ? 0.0 : w;
     }
 };
 
@@ -143,6 +147,21 @@ template <typename T>
 __device__ __forceinline__ u32x4 load_vector(const Grid<T>& z, int64_t at) {
     return at < z.vocab + z.shift ? *(const u32x4*)(z.origin + at) : u32x4{0, 0, 0, 0};
 }
+// The vector with -inf in the places outside the row.
+template <typename T>
+__device__ __forceinline__ u32x4 in_row(const Grid<T>& z, int64_t at, u32x4 raw) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) raw[e] = z.has(at + e) ? raw[e] : 0xff800000u;
+    } else {
+        const uint32_t none = __builtin_bit_cast(unsigned short, (T)-INFINITY);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!z.has(at + e)) raw[e / 2] = e % 2 ? (raw[e / 2] & 0xffffu) | none << 16 : (raw[e / 2] & 0xffff0000u) | none;
+    }
+    return raw;
+}
+__device__ __forceinline__ int32_t wave_of_block() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
 template <int kCtrl>
 __device__ __forceinline__ float dpp_max(float x) {
@@ -189,7 +208,7 @@ __global__ __launch_bounds__(kScanThreads) void asd_sample_scan_kernel(SampleArg
                                                                        int32_t tiles) {
     typedef typename Element<kType>::T T;
     constexpr int kPer = 16 / sizeof(T), kLoads = kGroup / (64 * kPer);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = wave_of_block();
     const int64_t row = blockIdx.x / tiles;
     const int32_t tile = (int32_t)(blockIdx.x - row * tiles);
     const Grid<T> z(a, row);
@@ -211,7 +230,10 @@ __global__ __launch_bounds__(kScanThreads) void asd_sample_scan_kernel(SampleArg
             next[l] = load_vector(z, (int64_t)(g + kScanWaves) * kGroup + (l * 64 + lane) * kPer);
         }
         const int64_t base = (int64_t)g * kGroup;
-        const bool inside = g > 0 && g + 1 < groups;         // every place is in the row
+        if (g == 0 || g + 1 >= groups) {         // some places are not in the row
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) raw[l] = in_row(z, base + (l * 64 + lane) * kPer, raw[l]);
+        }
         float top = -INFINITY;
         bool any_nan = false;
 #pragma unroll
@@ -222,9 +244,8 @@ __global__ __launch_bounds__(kScanThreads) void asd_sample_scan_kernel(SampleArg
             bool nan = false;
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
-                const float v = inside || z.has(base + (l * 64 + lane) * kPer + e) ? x[e] : -INFINITY;
-                nan |= v != v;
-                m = fmaxf(m, v);
+                nan |= x[e] != x[e];
+                m = fmaxf(m, x[e]);
             }
             m = dpp_max<kXor1>(m);
             m = dpp_max<kXor2>(m);
@@ -243,16 +264,25 @@ __global__ __launch_bounds__(kScanThreads) void asd_sample_scan_kernel(SampleArg
         top = across_rows_max(top);
         double sum = 0.0;
         if (whole) {
-            const double from = top == -INFINITY ? 0.0 : (double)top;
+            // A finite greatest logit weighs 1, so that the 2^-1000 of tokens far below, -inf among
+            // them, changes no sum; where it is +inf the tokens there share the weight.
+            if (top > -INFINITY && top < INFINITY) {
+                const double from = (double)top;
 #pragma unroll
-            for (int l = 0; l < kLoads; ++l) {
-                float x[kPer];
-                unpack<T>(raw[l], x);
+                for (int l = 0; l < kLoads; ++l) {
+                    float x[kPer];
+                    unpack<T>(raw[l], x);
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) {
-                    const bool in = inside || z.has(base + (l * 64 + lane) * kPer + e);
-                    const double w = power2(((double)x[e] - from) * per);
-                    sum += !in || x[e] == -INFINITY ? 0.0 : x[e] == top ? 1.0 : top == INFINITY ? 0.0 : w;
+                    for (int e = 0; e < kPer; ++e) sum += power2_clamped(((double)x[e] - from) * per);
+                }
+            } else if (top == INFINITY) {
+#pragma unroll
+                for (int l = 0; l < kLoads; ++l) {
+                    float x[kPer];
+                    unpack<T>(raw[l], x);
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e)
+                        sum += x[e] == INFINITY ? 1.0 : 0.0;
                 }
             }
             sum = wave_sum(sum);
@@ -306,6 +336,27 @@ template <int kN> struct Block {
         u64 all = 0;
         for (int w = 0; w < kWaves; ++w) all += u[w];
         return all;
+    }
+    // Sums with one barrier: of a number that each wavefront has, and of one that each thread has.  The
+    // place alternates, so that a wavefront that is ahead does not write what another still reads.
+    uint32_t votes_of[2][kWaves];
+    double masses_of[2][kWaves];
+    __device__ __forceinline__ uint32_t votes(uint32_t of_wave, int turn) {
+        if ((threadIdx.x & 63) == 0) votes_of[turn & 1][threadIdx.x >> 6] = of_wave;
+        __syncthreads();
+        uint32_t sum = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum += votes_of[turn & 1][w];
+        return sum;
+    }
+    __device__ __forceinline__ double mass(double v, int turn) {
+        v = wave_sum(v);
+        if ((threadIdx.x & 63) == 0) masses_of[turn & 1][threadIdx.x >> 6] = v;
+        __syncthreads();
+        double sum = 0.0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) sum += masses_of[turn & 1][w];
+        return sum;
     }
     // sum over the threads before this one, and over all
     template <typename V>
@@ -371,7 +422,8 @@ __device__ __forceinline__ float inside_unit(float u) {
 
 constexpr int kPickThreads = 256, kListed = 2048, kHeld = 16;
 constexpr int kMostSubs = kPickThreads * kHeld;          // sub-block maxima held in registers
-constexpr int kFewest = 512;                             // sub-blocks that candidates come from without top-k
+constexpr int kFewest = 192;                             // sub-blocks that candidates come from without top-k
+constexpr int kRanked = 2;                               // candidates a thread ranks by comparing each with each
 // Tokens that top-k may ask for here: as many sub-block maxima have to reach the threshold, which the
 // candidates then exceed by -ln(1 - k / subs) / (k / subs), 2.0 at 0.8, where the row is in no order.
 __device__ __forceinline__ int32_t most_k(int32_t subs) { return min(subs * 4 / 5, 1200); }
@@ -384,8 +436,9 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     __shared__ uint32_t key[kListed], place[kListed];
     __shared__ double weight[kListed];
     __shared__ int32_t wanted[kMostSubs / 2];
+    __shared__ uint32_t starts[kMostSubs / 2 * (kSub / kPer) / 64];
     __shared__ int32_t found;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_of_block();
     const int64_t row = blockIdx.x;
     const Grid<T> z(a, row);
     const Row r(a, row);
@@ -478,10 +531,14 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     uint32_t least = 0;         // by bisection over its upper 16 bits
     for (int bit = 31; bit >= 16; --bit) {
         const uint32_t trial = least | 1u << bit;
+        if (trial > top) continue;
         uint32_t n = 0;
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) n += held[i] >= trial;
-        if (block.count(n) >= (uint32_t)need) least = trial;
+        for (int i = 0; i < kHeld; ++i) {
+            if (i * kPickThreads >= subs) break;
+            n += (uint32_t)__popcll(__ballot(held[i] >= trial));
+        }
+        if (block.votes(n, bit) >= (uint32_t)need) least = trial;
     }
     least = max(least, kKeyNegInf);
     // the sub-blocks that reach it, in order
@@ -496,144 +553,184 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
         blocks += total;
     }
     __syncthreads();
-    // their tokens, in order
+    // Their tokens, in order: a sweep that counts them, 64 vectors at a time, and one that lists them (the
+    // second finds them in the L2); several loads of a wavefront are on the way at once.
     int32_t n = 0;
-    constexpr int kLanes = kSub / kPer, kAtOnce = kPickThreads / kLanes;
+    constexpr int kLanes = kSub / kPer, kAhead = 4, kWaves = kPickThreads / 64;
+    const int32_t sweeps = (blocks * kLanes + 63) / 64;
     if (blocks <= kMostSubs / 2) {
-        for (int32_t b = 0; b < blocks && n <= kListed; b += kAtOnce) {
-            const int32_t i = b + tid / kLanes;
-            int64_t at = 0;
-            uint32_t k[kPer];
-            int32_t mine = 0;
-            if (i < blocks) {
-                at = (int64_t)wanted[i] * kSub + tid % kLanes * kPer;
-                float x[kPer];
-                unpack<T>(load_vector(z, at), x);
+        const auto sweep = [&](auto&& f) {
+            for (int32_t b = wave; b < sweeps; b += kAhead * kWaves) {
+                u32x4 raw[kAhead];
+                int64_t at[kAhead];
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) {
-                    k[e] = z.has(at + e) ? key_of(x[e]) : 0;
-                    mine += k[e] >= least;
+                for (int c = 0; c < kAhead; ++c) {
+                    const int32_t v = (b + c * kWaves) * 64 + lane;
+                    at[c] = v < blocks * kLanes ? (int64_t)wanted[v / kLanes] * kSub + v % kLanes * kPer : -1;
+                    raw[c] = at[c] >= 0 ? load_vector(z, at[c]) : u32x4{0, 0, 0, 0};
+                }
+#pragma unroll
+                for (int c = 0; c < kAhead; ++c) {
+                    if (b + c * kWaves >= sweeps) break;
+                    float x[kPer];
+                    unpack<T>(raw[c], x);
+                    uint32_t k[kPer];
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) k[e] = at[c] >= 0 && z.has(at[c] + e) ? key_of(x[e]) : 0;
+                    f(b + c * kWaves, at[c], k);
                 }
             }
+        };
+        sweep([&](int32_t b, int64_t, const uint32_t* k) {
+            uint32_t c = 0;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) c += (uint32_t)__popcll(__ballot(k[e] >= least));
+            if (lane == 0) starts[b] = c;
+        });
+        __syncthreads();
+        for (int32_t b0 = 0; b0 < sweeps; b0 += kPickThreads) {
+            const int32_t c = b0 + tid < sweeps ? (int32_t)starts[b0 + tid] : 0;
             int32_t total;
-            int32_t to = n + block.before(mine, (int32_t*)block.u, &total);
-            if (i < blocks) {
+            const int32_t before = n + block.before(c, (int32_t*)block.u, &total);
+            if (b0 + tid < sweeps) starts[b0 + tid] = (uint32_t)before;
+            n += total;
+        }
+        __syncthreads();
+        if (n <= kListed)
+            sweep([&](int32_t b, int64_t at, const uint32_t* k) {
+                uint32_t to = starts[b];
+                const u64 below = (1ull << lane) - 1;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) to += (uint32_t)__popcll(__ballot(k[e] >= least) & below);
 #pragma unroll
                 for (int e = 0; e < kPer; ++e)
                     if (k[e] >= least) {
-                        if (to < kListed) {
-                            key[to] = k[e];
-                            place[to] = (uint32_t)(at + e);
-                        }
+                        key[to] = k[e];
+                        place[to] = (uint32_t)(at + e);
                         ++to;
                     }
-            }
-            n += total;
-        }
+            });
     }
     if (blocks > kMostSubs / 2 || n > kListed) {
         if (tid == 0) s.flat[row] = 1;
         return;
     }
     __syncthreads();
-    double sum = 0.0;
-    for (int i = tid; i < n; i += kPickThreads) sum += weight[i] = w(value_of(key[i]));
-    // (every thread keeps to the candidates tid, tid + 256, ...; sums over them are the block's, in one order)
-
-    // The greatest key that enough tokens, or tokens of enough weight, reach; the first `ties` of
-    // those that have it are kept.
-    uint32_t cut = 0;
-    int32_t ties = 0x7fffffff;
-    if (r.by_count) {
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t trial = cut | 1u << bit;
-            uint32_t c = 0;
-            for (int i = tid; i < n; i += kPickThreads) c += key[i] >= trial;
-            if (block.count(c) >= (uint32_t)r.k) cut = trial;
-        }
-        uint32_t c = 0;
-        double mine = 0.0;
-        for (int i = tid; i < n; i += kPickThreads)
-            if (key[i] > cut) {
-                ++c;
-                mine += weight[i];
-            }
-        ties = r.k - (int32_t)block.count(c);
-        all = block.sum(mine) + ties * w(value_of(cut));
-    } else {
-        sum = block.sum(sum);
-        const bool everything = least == kKeyNegInf;        // no token is left out
-        if (!everything && !(r.by_mass && sum >= (double)r.p * all) &&
-            !(r.by_floor && w(value_of(least)) < (double)r.m)) {
-            if (tid == 0) s.flat[row] = 1;
-            return;
-        }
-        // (where the floor alone bounds the candidates, the nucleus may be larger than they are: all of them)
-        if (!everything && r.by_mass && sum < (double)r.p * all) cut = least;
-    }
-    if (r.by_mass && (r.by_count || cut == 0)) {
-        const double goal = (double)r.p * all;
-        const uint32_t limit = cut;
-        const int32_t limit_ties = ties;
-        // tokens at `limit` beyond its ties do not count
-        uint32_t same = 0;
-        if (r.by_count) {
-            uint32_t c = 0;
-            for (int i = tid; i < n; i += kPickThreads) c += key[i] == limit;
-            same = block.count(c);
-        }
-        const double beyond = r.by_count ? ((int32_t)same - limit_ties) * w(value_of(limit)) : 0.0;
-        uint32_t t = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t trial = t | 1u << bit;
-            double mine = 0.0;
-            for (int i = tid; i < n; i += kPickThreads)
-                if (key[i] >= trial) mine += weight[i];
-            const double reach = block.sum(mine) - (trial <= limit ? beyond : 0.0);
-            if (reach >= goal && reach > 0.0) t = trial;
-        }
-        if (t > limit || !r.by_count) {
-            double mine = 0.0;
-            for (int i = tid; i < n; i += kPickThreads)
-                if (key[i] > t) mine += weight[i];
-            const double above = block.sum(mine), one = w(value_of(t));
-            cut = t;
-            ties = max(1, one > 0.0 ? (int32_t)min(ceil((goal - above) / one), 2e9) : 1);
-        } else {
-            double mine = 0.0;
-            for (int i = tid; i < n; i += kPickThreads)
-                if (key[i] > limit) mine += weight[i];
-            const double above = block.sum(mine), one = w(value_of(limit));
-            ties = min(limit_ties, max(1, one > 0.0 ? (int32_t)min(ceil((goal - above) / one), 2e9) : 1));
-        }
+    double mine = 0.0;
+    for (int i = tid; i < n; i += kPickThreads) mine += weight[i] = w(value_of(key[i]));
+    const double floor = r.by_floor ? (double)r.m : 0.0, sum = block.sum(mine);
+    if (!r.by_count && least != kKeyNegInf &&            // some tokens are no candidates
+        !(r.by_mass && sum >= (double)r.p * all) && !(r.by_floor && w(value_of(least)) < floor)) {
+        if (tid == 0) s.flat[row] = 1;
+        return;
     }
 
-    // What is kept, in order, and the draw.  (A thread takes neighbouring candidates.)
-    const double floor = r.by_floor ? (double)r.m : 0.0;
     const int each = (n + kPickThreads - 1) / kPickThreads, from = min(n, tid * each), to = min(n, from + each);
-    int32_t at_cut = 0, total_cut;
-    for (int i = from; i < to; ++i) at_cut += key[i] == cut;
-    at_cut = block.before(at_cut, (int32_t*)block.u, &total_cut);
-    const auto kept = [&](int i, int32_t& seen) {
-        if (key[i] < cut || (key[i] == cut && seen++ >= ties)) return 0.0;
-        return weight[i] >= floor ? weight[i] : 0.0;
-    };
-    int32_t seen = at_cut;
-    double mine = 0.0, total;
-    for (int i = from; i < to; ++i) mine += kept(i, seen);
+    if (n <= kRanked * kPickThreads) {
+        // Few: a candidate's rank, and the weight of those ranked before it, by comparing it with each.
+        uint32_t own[kRanked], rank[kRanked];
+        double before[kRanked];
+#pragma unroll
+        for (int c = 0; c < kRanked; ++c) {
+            const int i = c * kPickThreads + tid;
+            own[c] = i < n ? key[i] : 0;
+            rank[c] = 0;
+            before[c] = 0.0;
+        }
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            const uint32_t k = key[i];
+            const double x = weight[i];
+#pragma unroll
+            for (int c = 0; c < kRanked; ++c) {
+                const bool first = k > own[c] || (k == own[c] && i < c * kPickThreads + tid);
+                rank[c] += first;
+                before[c] += first ? x : 0.0;
+            }
+        }
+        double kept[kRanked], mine = 0.0;
+#pragma unroll
+        for (int c = 0; c < kRanked; ++c) {
+            const int i = c * kPickThreads + tid;
+            kept[c] = i < n && (!r.by_count || rank[c] < (uint32_t)r.k) ? weight[i] : 0.0;
+            mine += kept[c];
+        }
+        if (r.by_count) all = block.sum(mine);
+        const double goal = (double)r.p * all;
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < kRanked; ++c) {
+            const int i = c * kPickThreads + tid;
+            if (i < n)
+                weight[i] = kept[c] >= floor && (!r.by_mass || rank[c] == 0 || before[c] < goal) ? kept[c] : 0.0;
+        }
+    } else {
+        // The greatest key that enough tokens, or tokens of enough weight, reach, bit by bit from the first
+        // in which the candidates differ; the first `ties` of those that have it are kept.
+        const int first_bit = top == least ? -1 : 31 - __builtin_clz(top ^ least);
+        const uint32_t common = first_bit == 31 ? 0u : top & ~((2u << max(first_bit, 0)) - 1u);
+        const uint32_t start = first_bit < 0 ? top : common;
+        const auto above = [&](uint32_t bound, int turn) {          // weight of the keys greater than it
+            double x = 0.0;
+            for (int i = tid; i < n; i += kPickThreads)
+                if (key[i] > bound) x += weight[i];
+            return block.mass(x, turn);
+        };
+        const auto reaching = [&](uint32_t bound, int turn) {       // tokens whose keys reach it
+            uint32_t c = 0;
+            for (int i = 0; i < n; i += kPickThreads)
+                c += (uint32_t)__popcll(__ballot(i + tid < n && key[i + tid] >= bound));
+            return block.votes(c, turn);
+        };
+        uint32_t cut = 0;
+        int32_t ties = 0x7fffffff;
+        double beyond = 0.0;                // weight of the tokens at the count's cut that it leaves out
+        if (r.by_count) {
+            cut = start;
+            for (int bit = first_bit; bit >= 0; --bit)
+                if (reaching(cut | 1u << bit, bit) >= (uint32_t)r.k) cut |= 1u << bit;
+            const int32_t more = (int32_t)reaching(cut + 1, 1);
+            ties = r.k - more;
+            const double one = w(value_of(cut));
+            beyond = ((int32_t)reaching(cut, 0) - r.k) * one;
+            all = above(cut, 0) + ties * one;
+        }
+        if (r.by_mass && (r.by_count || sum >= (double)r.p * all)) {
+            const double goal = (double)r.p * all;
+            uint32_t t = start;
+            for (int bit = first_bit; bit >= 0; --bit) {
+                const uint32_t trial = t | 1u << bit;
+                const double reach = above(trial - 1, bit) - (trial <= cut ? beyond : 0.0);
+                if (reach >= goal && reach > 0.0) t = trial;
+            }
+            const double one = w(value_of(t)), missing = goal - above(t, 1);
+            const int32_t m = max(1, one > 0.0 ? (int32_t)min(ceil(missing / one), 2e9) : 1);
+            ties = t == cut ? min(ties, m) : m;
+            cut = t;
+        }
+        int32_t seen = 0, total_cut;
+        for (int i = from; i < to; ++i) seen += key[i] == cut;
+        seen = block.before(seen, (int32_t*)block.u, &total_cut);
+        for (int i = from; i < to; ++i)
+            if (key[i] < cut || (key[i] == cut && seen++ >= ties) || weight[i] < floor) weight[i] = 0.0;
+    }
+    __syncthreads();
+
+    // The draw, in order: a thread takes neighbouring candidates.
+    mine = 0.0;
+    for (int i = from; i < to; ++i) mine += weight[i];
+    double total;
     const double before = block.before(mine, block.d, &total), target = (double)u * total;
     uint32_t passes = block.min(mine > 0.0 && before + mine > target ? (uint32_t)tid : ~0u);
     if (passes == ~0u) passes = block.max(mine > 0.0 ? (uint32_t)tid : 0u);
     if ((uint32_t)tid == passes) {
-        seen = at_cut;
         double run = before, x = 0.0;
         int at = from;
         for (int i = from; i < to; ++i) {
-            const double y = kept(i, seen);
-            run += y;
-            if (y > 0.0) {
+            run += weight[i];
+            if (weight[i] > 0.0) {
                 at = i;
-                x = y;
+                x = weight[i];
                 if (run > target) break;
             }
         }
@@ -665,12 +762,12 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
     __shared__ Block<kFlatThreads> block;
     __shared__ u64 bin_weight[kBins];
     __shared__ uint32_t bin_count[kBins];
-    __shared__ uint32_t key[kCollected];
+    __shared__ uint32_t key[kCollected], place[kCollected];
     __shared__ u64 span_sum[kSpans];
     __shared__ uint32_t span_ties[kSpans];
     __shared__ uint32_t collected;
     __shared__ u64 pick[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_of_block();
     const int64_t row = blockIdx.x;
     if (s.flat[row] == 0) return;
     const Grid<T> z(a, row);
@@ -698,6 +795,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
                 raw[l] = next[l];
                 next[l] = load_vector(z, (int64_t)(g + kFlatWaves) * kGroup + (l * 64 + lane) * kPer);
             }
+            const bool edge = g == 0 || g + 1 >= groups;
 #pragma unroll
             for (int l = 0; l < kLoads; ++l) {
                 float x[kPer];
@@ -705,154 +803,239 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
                 const int64_t at = (int64_t)g * kGroup + (l * 64 + lane) * kPer;
 #pragma unroll
                 for (int e = 0; e < kPer; ++e)
-                    if (z.has(at + e)) f(key_of(x[e]), x[e], at + e);
+                    if (!edge || z.has(at + e)) f(key_of(x[e]), x[e], at + e);
             }
             end(g);
         }
     };
     const auto nothing = [](int32_t) {};
 
+    // What every span holds: the weights of the tokens whose order exceeds `at_order`, and, of those that have
+    // it, the tokens themselves (key and place), or, where the order is the whole key, how many there are.
+    const auto survey = [&](auto&& order, uint32_t at_order, bool whole_key, uint32_t limit) {
+        for (int i = tid; i < kSpans; i += kFlatThreads) {
+            span_sum[i] = 0;
+            span_ties[i] = 0;
+        }
+        if (tid == 0) collected = 0;
+        __syncthreads();
+        u64 mine = 0;
+        uint32_t same = 0;
+        over(
+            [&](uint32_t k, float x, int64_t at) {
+                const uint32_t b = order(k, x);
+                if (b > at_order) {
+                    const double real = w(x);
+                    mine += real >= least ? fixed(real) : 0;
+                } else if (b == at_order && k >= limit) {
+                    if (whole_key) {
+                        ++same;
+                    } else {
+                        const uint32_t i = atomicAdd(&collected, 1u);
+                        if (i < kCollected) {
+                            key[i] = k;
+                            place[i] = (uint32_t)at;
+                        }
+                    }
+                }
+            },
+            [&](int32_t g) {
+                for (int x = 32; x > 0; x >>= 1) {
+                    mine += (u64)__shfl_xor((long long)mine, x);
+                    same += (uint32_t)__shfl_xor((int)same, x);
+                }
+                if (lane == 0) {
+                    atomicAdd(&span_sum[g / per_span], mine);
+                    atomicAdd(&span_ties[g / per_span], same);
+                }
+                mine = 0;
+                same = 0;
+            });
+        __syncthreads();
+    };
+    const auto clear_bins = [&]() {
+        for (int b = tid; b < kBins; b += kFlatThreads) {
+            bin_weight[b] = 0;
+            bin_count[b] = 0;
+        }
+        __syncthreads();
+    };
+    // The bin in which `want` is reached, from the last one down, and what is still wanted of it: four bins a thread.
+    const auto find_bin = [&](bool weights, u64* want) -> uint32_t {
+        u64 four[4], mine = 0, total;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int b = kBins - 1 - (4 * tid + i);
+            four[i] = weights ? bin_weight[b] : bin_count[b];
+            mine += four[i];
+        }
+        u64 have = block.before(mine, block.u, &total);
+        if (tid == 0) {
+            pick[0] = 0;
+            pick[1] = *want;
+        }
+        __syncthreads();
+        if (have < *want && have + mine >= *want) {
+            for (int i = 0; i < 4; ++i) {
+                if (have + four[i] >= *want) {
+                    pick[0] = (u64)(kBins - 1 - (4 * tid + i));
+                    pick[1] = *want - have;
+                    break;
+                }
+                have += four[i];
+            }
+        }
+        __syncthreads();
+        const uint32_t bin = (uint32_t)pick[0];
+        *want = pick[1];
+        __syncthreads();
+        return bin;
+    };
+
     // Keys above `cut` are kept, and the first `ties` tokens that have it; stage 0 cuts by count, stage 1 by
     // mass among what stage 0 left.
     uint32_t cut = 0;
     u64 ties = ~0ull;
+    // Bins of 1/64 octave of the weight, the last one for all below 2^-64: tokens spread over many of them, so
+    // that few add to one at a time.  (Leading bits of the keys put a row of N(0, 2) into some
+    // sixty: its histogram alone took 70 us.)
+    const float steps = (float)(64.0 * w.per);
+    const auto near_top = [&](uint32_t, float x) -> uint32_t {
+        return (uint32_t)(kBins - 1) - min((uint32_t)((w.top_f - x) * steps), (uint32_t)(kBins - 1));
+    };
     for (int stage = 0; stage < 2; ++stage) {
         if (!(stage == 0 ? r.by_count : r.by_mass)) continue;
+        const bool by_weight = stage == 1;
         const uint32_t limit = cut;
         const u64 limit_ties = ties, limit_weight = limit ? fixed(w(value_of(limit))) : 0;
+        const u64 limit_mass = by_weight && limit != 0 ? limit_ties * limit_weight : 0;
+        const auto worth = [&](uint32_t k) -> u64 {      // of a token beyond the limit's
+            return !by_weight ? 1 : k > limit ? fixed(w(value_of(k))) : 0;
+        };
         u64 want = (u64)r.k;
-        uint32_t prefix = 0;            // of the cut's key, from bit `shift` up
-        int shift = 32;
-        u64 in_bin = 0;
-        while (shift > 0) {
-            const int low = shift == 32 ? 20 : shift == 20 ? 8 : 0;
-            const uint32_t mask = (1u << (shift - low)) - 1;
-            for (int b = tid; b < kBins; b += kFlatThreads) {
-                bin_weight[b] = 0;
-                bin_count[b] = 0;
-            }
-            __syncthreads();
+        bool listed = false, limit_in = false;        // a list, and the limit's tokens in it
+        if (top < kKeyInf) {
+            clear_bins();
             over(
                 [&](uint32_t k, float x, int64_t) {
-                    if (k < limit || (shift < 32 && k >> shift != prefix)) return;
-                    const uint32_t b = k >> low & mask;
-                    if (stage == 1 && k > limit) atomicAdd(&bin_weight[b], fixed(w(x)));
-                    atomicAdd(&bin_count[b], 1u);
+                    if (k < limit) return;
+                    const uint32_t b = near_top(k, x);
+                    if (!by_weight) atomicAdd(&bin_count[b], 1u);
+                    else if (k > limit) atomicAdd(&bin_weight[b], fixed(w(x)));
                 },
                 nothing);
             __syncthreads();
             // of the tokens at the limit only those count that stage 0 kept
-            if (stage == 1 && limit != 0 && (shift == 32 || limit >> shift == prefix) && tid == 0)
-                bin_weight[limit >> low & mask] += limit_ties * limit_weight;
+            if (limit_mass != 0 && tid == 0) bin_weight[near_top(limit, value_of(limit))] += limit_mass;
             __syncthreads();
-            if (stage == 1 && shift == 32) {
+            if (by_weight) {
                 u64 mine = 0;
                 for (int b = tid; b < kBins; b += kFlatThreads) mine += bin_weight[b];
                 want = max((u64)1, share(r.p, block.sum(mine), true));
             }
-            // the bin in which the wanted amount is reached, from the greatest key down: four bins a thread
-            u64 four[4], mine = 0, total;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int b = kBins - 1 - (4 * tid + i);
-                four[i] = stage == 1 ? bin_weight[b] : bin_count[b];
-                mine += four[i];
-            }
-            u64 have = block.before(mine, block.u, &total);
-            if (tid == 0) {         // none: the last token there is
-                pick[0] = 0;
-                pick[1] = want;
-            }
-            __syncthreads();
-            if (have < want && have + mine >= want) {
-                for (int i = 0; i < 4; ++i) {
-                    if (have + four[i] >= want) {
-                        pick[0] = (u64)(kBins - 1 - (4 * tid + i));
-                        pick[1] = want - have;
-                        break;
-                    }
-                    have += four[i];
-                }
-            }
-            __syncthreads();
-            prefix = (shift == 32 ? 0u : prefix << (shift - low)) | (uint32_t)pick[0];
-            want = pick[1];
-            in_bin = bin_count[pick[0]];
-            shift = low;
-            __syncthreads();
-            if (in_bin <= (u64)kCollected) break;
+            u64 rest = want;
+            const uint32_t bin = find_bin(by_weight, &rest);
+            survey(near_top, bin, false, limit);
+            listed = collected <= (uint32_t)kCollected;
+            if (listed) want = rest;
+            limit_in = limit_mass != 0 && near_top(limit, value_of(limit)) == bin;
         }
-        if (shift > 0) {
-            // the bin's tokens, and the cut among them
-            if (tid == 0) collected = 0;
-            __syncthreads();
-            over(
-                [&](uint32_t k, float, int64_t at) {
-                    if (k >= limit && k >> shift == prefix) {
-                        const uint32_t i = atomicAdd(&collected, 1u);
-                        if (i < kCollected) key[i] = k;
-                    }
-                },
-                nothing);
-            __syncthreads();
-            const int n = min((int)collected, kCollected);
-            const bool limit_in = stage == 1 && limit != 0 && limit >> shift == prefix;
-            for (int bit = shift - 1; bit >= 0; --bit) {
-                const uint32_t trial = (prefix << (shift - bit) | 1u) << bit;
+        uint32_t prefix = 0;            // of the cut's key, from bit `shift` up
+        int shift = 32;
+        if (!listed) {
+            // More tokens in one bin than the list holds: by the keys' bits.
+            if (by_weight && !(top < kKeyInf)) {
                 u64 mine = 0;
-                for (int i = tid; i < n; i += kFlatThreads) {
-                    if (key[i] < trial) continue;
-                    mine += stage == 0 ? 1 : key[i] > limit ? fixed(w(value_of(key[i]))) : 0;
+                over([&](uint32_t k, float x, int64_t) { mine += k > limit ? fixed(w(x)) : 0; }, nothing);
+                want = max((u64)1, share(r.p, block.sum(mine) + limit_mass, true));
+            }
+            u64 in_bin = ~0ull;
+            while (shift > 0 && in_bin > (u64)kCollected) {
+                const int low = shift == 32 ? 20 : shift == 20 ? 8 : 0;
+                const uint32_t mask = (1u << (shift - low)) - 1;
+                clear_bins();
+                over(
+                    [&](uint32_t k, float x, int64_t) {
+                        if (k < limit || (shift < 32 && k >> shift != prefix)) return;
+                        const uint32_t b = k >> low & mask;
+                        if (by_weight && k > limit) atomicAdd(&bin_weight[b], fixed(w(x)));
+                        atomicAdd(&bin_count[b], 1u);
+                    },
+                    nothing);
+                __syncthreads();
+                if (limit_mass != 0 && (shift == 32 || limit >> shift == prefix) && tid == 0)
+                    bin_weight[limit >> low & mask] += limit_mass;
+                __syncthreads();
+                const uint32_t bin = find_bin(by_weight, &want);
+                in_bin = bin_count[bin];
+                prefix = (shift == 32 ? 0u : prefix << (shift - low)) | bin;
+                shift = low;
+                __syncthreads();
+            }
+            survey([&](uint32_t k, float) { return k >> shift; }, prefix, shift == 0, limit);
+            listed = shift > 0;
+            limit_in = limit_mass != 0 && listed && limit >> shift == prefix;
+        }
+        if (listed) {
+            // the cut among the listed tokens
+            const int n = min((int)collected, kCollected);
+            if (n <= kFlatThreads) {
+                // a token's rank and the worth of those before it, by comparing it with each
+                const uint32_t k = tid < n ? key[tid] : 0, at = tid < n ? place[tid] : 0;
+                u64 before = 0;
+                uint32_t same_before = 0;
+                for (int i = 0; i < n; ++i) {
+                    const uint32_t other = key[i];
+                    const bool same = other == k && place[i] < at;
+                    if (other > k || same) before += worth(other);
+                    same_before += same;
                 }
-                u64 reach = block.sum(mine);
-                if (limit_in && trial <= limit) reach += limit_ties * limit_weight;
-                prefix = prefix << 1 | (reach >= want ? 1u : 0u);
-                shift = bit;
+                const bool at_limit = by_weight && limit != 0 && k == limit;
+                if (at_limit) before += min((u64)same_before, limit_ties) * limit_weight;
+                const bool kept = tid < n && before < want && !(at_limit && same_before >= limit_ties);
+                prefix = block.min(kept ? k : ~0u);
+                want = block.count(kept && k == prefix);
+                cut = prefix;
+                ties = want;
+            } else {
+                prefix = shift == 32 ? 0u : prefix;
+                while (shift > 0) {
+                    const uint32_t trial = (prefix << 1 | 1u) << (shift - 1);
+                    u64 mine = 0;
+                    for (int i = tid; i < n; i += kFlatThreads)
+                        if (key[i] >= trial) mine += worth(key[i]);
+                    u64 reach = block.sum(mine);
+                    if (limit_in && trial <= limit) reach += limit_mass;
+                    prefix = prefix << 1 | (reach >= want ? 1u : 0u);
+                    --shift;
+                }
+                u64 mine = 0;
+                for (int i = tid; i < n; i += kFlatThreads)
+                    if (key[i] > prefix) mine += worth(key[i]);
+                want -= min(want, block.sum(mine));
+                const u64 one = by_weight ? fixed(w(value_of(prefix))) : 1;
+                const u64 m = max((u64)1, one > 0 ? (want + one - 1) / one : 1);
+                ties = by_weight && prefix == limit ? min(m, limit_ties) : m;
+                cut = prefix;
             }
-            u64 mine = 0;
-            for (int i = tid; i < n; i += kFlatThreads)
-                if (key[i] > prefix) mine += stage == 0 ? 1 : key[i] > limit ? fixed(w(value_of(key[i]))) : 0;
-            want -= min(want, block.sum(mine));
-        }
-        cut = prefix;
-        if (stage == 0) {
-            ties = want;
+            for (int i = tid; i < n; i += kFlatThreads) {
+                const int32_t span = (int32_t)(place[i] / (uint32_t)kGroup) / per_span;
+                if (key[i] > cut) {
+                    const double real = w(value_of(key[i]));
+                    if (real >= least) atomicAdd(&span_sum[span], fixed(real));
+                } else if (key[i] == cut) {
+                    atomicAdd(&span_ties[span], 1u);
+                }
+            }
+            __syncthreads();
         } else {
-            const u64 one = fixed(w(value_of(cut)));
+            cut = prefix;
+            const u64 one = by_weight ? fixed(w(value_of(cut))) : 1;
             const u64 m = max((u64)1, one > 0 ? (want + one - 1) / one : 1);
-            ties = cut == limit ? min(m, limit_ties) : m;
+            ties = by_weight && cut == limit ? min(m, limit_ties) : m;
         }
     }
-
-    // What every span keeps: the weights above the cut, and how many tokens have its key.
-    for (int i = tid; i < kSpans; i += kFlatThreads) {
-        span_sum[i] = 0;
-        span_ties[i] = 0;
-    }
-    __syncthreads();
-    u64 mine = 0;
-    uint32_t same = 0;
-    over(
-        [&](uint32_t k, float x, int64_t) {
-            if (k > cut) {
-                const double real = w(x);
-                mine += real >= least ? fixed(real) : 0;
-            }
-            same += k == cut;
-        },
-        [&](int32_t g) {
-            for (int x = 32; x > 0; x >>= 1) {
-                mine += (u64)__shfl_xor((long long)mine, x);
-                same += (uint32_t)__shfl_xor((int)same, x);
-            }
-            if (lane == 0) {
-                atomicAdd(&span_sum[g / per_span], mine);
-                atomicAdd(&span_ties[g / per_span], same);
-            }
-            mine = 0;
-            same = 0;
-        });
-    __syncthreads();
+    if (!r.by_count && !r.by_mass) survey([](uint32_t k, float) { return k; }, 0, true, 0);
     const double cut_real = w(value_of(cut));
     const u64 cut_weight = cut_real >= least ? fixed(cut_real) : 0;
     const u64 here = tid < spans ? span_ties[tid] : 0;
