@@ -778,10 +778,23 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
     for (int32_t g = tid; g < groups; g += kFlatThreads) top = max(top, s.tops[row * s.groups + g]);
     top = block.max(top);
     const Weights w(value_of(top), r.t);
-    const double unit = (double)(1ull << bits), least = r.by_floor ? (double)r.m : 0.0;
-    const auto fixed = [&](double x) { return (u64)(x * unit + 0.5); };
+    const double unit = (double)(1ull << bits);
+    // A weight as a whole number of units: added to 2^(52 - bits) it is rounded to one, which then stands in the
+    // sum's low bits.  (A weight below half a unit gives 0, as -inf does.)
+    const double carrier = (double)(1ull << (52 - bits));
+    const auto fixed = [&](double x) { return __builtin_bit_cast(u64, x + carrier) - __builtin_bit_cast(u64, carrier); };
+    const bool finite = top < kKeyInf;          // the greatest logit: then no token needs care
+    const auto weight_of = [&](float z) -> u64 {
+        return fixed(finite ? power2_clamped(((double)z - w.top) * w.per) : w(z));
+    };
+    // min-p in units: a weight counts from there on.  (Rounded up; the greatest token's always does.)
+    const u64 floor = r.by_floor ? (u64)ceil((double)r.m * unit) : 0;
+    const auto kept_weight = [&](float z) -> u64 {
+        const u64 x = weight_of(z);
+        return x >= floor ? x : 0;
+    };
 
-    // Calls f(key, value, grid place) for every token of the row, group by group, a wavefront each; a group's
+    // Calls f(value, grid place) for every token of the row, group by group, a wavefront each; a group's
     // end is told by end(group).
     const auto over = [&](auto&& f, auto&& end) {
         constexpr int kLoads = kGroup / (64 * kPer);
@@ -803,7 +816,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
                 const int64_t at = (int64_t)g * kGroup + (l * 64 + lane) * kPer;
 #pragma unroll
                 for (int e = 0; e < kPer; ++e)
-                    if (!edge || z.has(at + e)) f(key_of(x[e]), x[e], at + e);
+                    if (!edge || z.has(at + e)) f(x[e], at + e);
             }
             end(g);
         }
@@ -822,12 +835,13 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
         u64 mine = 0;
         uint32_t same = 0;
         over(
-            [&](uint32_t k, float x, int64_t at) {
-                const uint32_t b = order(k, x);
+            [&](float x, int64_t at) {
+                const uint32_t b = order(x);
                 if (b > at_order) {
-                    const double real = w(x);
-                    mine += real >= least ? fixed(real) : 0;
-                } else if (b == at_order && k >= limit) {
+                    mine += kept_weight(x);
+                } else if (b == at_order) {
+                    const uint32_t k = key_of(x);
+                    if (k < limit) return;
                     if (whole_key) {
                         ++same;
                     } else {
@@ -900,33 +914,32 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
     // that few add to one at a time.  (Leading bits of the keys put a row of N(0, 2) into some
     // sixty: its histogram alone took 70 us.)
     const float steps = (float)(64.0 * w.per);
-    const auto near_top = [&](uint32_t, float x) -> uint32_t {
+    const auto near_top = [&](float x) -> uint32_t {
         return (uint32_t)(kBins - 1) - min((uint32_t)((w.top_f - x) * steps), (uint32_t)(kBins - 1));
     };
     for (int stage = 0; stage < 2; ++stage) {
         if (!(stage == 0 ? r.by_count : r.by_mass)) continue;
         const bool by_weight = stage == 1;
         const uint32_t limit = cut;
-        const u64 limit_ties = ties, limit_weight = limit ? fixed(w(value_of(limit))) : 0;
+        const u64 limit_ties = ties, limit_weight = limit ? weight_of(value_of(limit)) : 0;
         const u64 limit_mass = by_weight && limit != 0 ? limit_ties * limit_weight : 0;
         const auto worth = [&](uint32_t k) -> u64 {      // of a token beyond the limit's
-            return !by_weight ? 1 : k > limit ? fixed(w(value_of(k))) : 0;
+            return !by_weight ? 1 : k > limit ? weight_of(value_of(k)) : 0;
         };
         u64 want = (u64)r.k;
         bool listed = false, limit_in = false;        // a list, and the limit's tokens in it
         if (top < kKeyInf) {
             clear_bins();
             over(
-                [&](uint32_t k, float x, int64_t) {
-                    if (k < limit) return;
-                    const uint32_t b = near_top(k, x);
+                [&](float x, int64_t) {
+                    const uint32_t b = near_top(x);
                     if (!by_weight) atomicAdd(&bin_count[b], 1u);
-                    else if (k > limit) atomicAdd(&bin_weight[b], fixed(w(x)));
+                    else if (limit == 0 || key_of(x) > limit) atomicAdd(&bin_weight[b], weight_of(x));
                 },
                 nothing);
             __syncthreads();
             // of the tokens at the limit only those count that stage 0 kept
-            if (limit_mass != 0 && tid == 0) bin_weight[near_top(limit, value_of(limit))] += limit_mass;
+            if (limit_mass != 0 && tid == 0) bin_weight[near_top(value_of(limit))] += limit_mass;
             __syncthreads();
             if (by_weight) {
                 u64 mine = 0;
@@ -938,7 +951,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
             survey(near_top, bin, false, limit);
             listed = collected <= (uint32_t)kCollected;
             if (listed) want = rest;
-            limit_in = limit_mass != 0 && near_top(limit, value_of(limit)) == bin;
+            limit_in = limit_mass != 0 && near_top(value_of(limit)) == bin;
         }
         uint32_t prefix = 0;            // of the cut's key, from bit `shift` up
         int shift = 32;
@@ -946,7 +959,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
             // More tokens in one bin than the list holds: by the keys' bits.
             if (by_weight && !(top < kKeyInf)) {
                 u64 mine = 0;
-                over([&](uint32_t k, float x, int64_t) { mine += k > limit ? fixed(w(x)) : 0; }, nothing);
+                over([&](float x, int64_t) { mine += key_of(x) > limit ? weight_of(x) : 0; }, nothing);
                 want = max((u64)1, share(r.p, block.sum(mine) + limit_mass, true));
             }
             u64 in_bin = ~0ull;
@@ -955,10 +968,11 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
                 const uint32_t mask = (1u << (shift - low)) - 1;
                 clear_bins();
                 over(
-                    [&](uint32_t k, float x, int64_t) {
+                    [&](float x, int64_t) {
+                        const uint32_t k = key_of(x);
                         if (k < limit || (shift < 32 && k >> shift != prefix)) return;
                         const uint32_t b = k >> low & mask;
-                        if (by_weight && k > limit) atomicAdd(&bin_weight[b], fixed(w(x)));
+                        if (by_weight && k > limit) atomicAdd(&bin_weight[b], weight_of(x));
                         atomicAdd(&bin_count[b], 1u);
                     },
                     nothing);
@@ -972,7 +986,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
                 shift = low;
                 __syncthreads();
             }
-            survey([&](uint32_t k, float) { return k >> shift; }, prefix, shift == 0, limit);
+            survey([&](float x) { return key_of(x) >> shift; }, prefix, shift == 0, limit);
             listed = shift > 0;
             limit_in = limit_mass != 0 && listed && limit >> shift == prefix;
         }
@@ -1013,7 +1027,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
                 for (int i = tid; i < n; i += kFlatThreads)
                     if (key[i] > prefix) mine += worth(key[i]);
                 want -= min(want, block.sum(mine));
-                const u64 one = by_weight ? fixed(w(value_of(prefix))) : 1;
+                const u64 one = by_weight ? weight_of(value_of(prefix)) : 1;
                 const u64 m = max((u64)1, one > 0 ? (want + one - 1) / one : 1);
                 ties = by_weight && prefix == limit ? min(m, limit_ties) : m;
                 cut = prefix;
@@ -1021,8 +1035,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
             for (int i = tid; i < n; i += kFlatThreads) {
                 const int32_t span = (int32_t)(place[i] / (uint32_t)kGroup) / per_span;
                 if (key[i] > cut) {
-                    const double real = w(value_of(key[i]));
-                    if (real >= least) atomicAdd(&span_sum[span], fixed(real));
+                    atomicAdd(&span_sum[span], kept_weight(value_of(key[i])));
                 } else if (key[i] == cut) {
                     atomicAdd(&span_ties[span], 1u);
                 }
@@ -1030,14 +1043,13 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
             __syncthreads();
         } else {
             cut = prefix;
-            const u64 one = by_weight ? fixed(w(value_of(cut))) : 1;
+            const u64 one = by_weight ? weight_of(value_of(cut)) : 1;
             const u64 m = max((u64)1, one > 0 ? (want + one - 1) / one : 1);
             ties = by_weight && cut == limit ? min(m, limit_ties) : m;
         }
     }
-    if (!r.by_count && !r.by_mass) survey([](uint32_t k, float) { return k; }, 0, true, 0);
-    const double cut_real = w(value_of(cut));
-    const u64 cut_weight = cut_real >= least ? fixed(cut_real) : 0;
+    if (!r.by_count && !r.by_mass) survey([](float x) { return key_of(x); }, 0, true, 0);
+    const u64 cut_weight = cut != 0 ? kept_weight(value_of(cut)) : 0;
     const u64 here = tid < spans ? span_ties[tid] : 0;
     u64 total;
     const u64 ties_before = block.before(here, block.u, &total);
@@ -1050,10 +1062,10 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
         uint32_t first = ~0u;
         double weight = 0.0;
         over(
-            [&](uint32_t k, float x, int64_t at) {
-                if (k < cut || first != ~0u) return;
+            [&](float x, int64_t at) {
+                if (key_of(x) < cut || first != ~0u) return;
                 const double real = w(x);
-                if (real > 0.0 && real >= least) {
+                if (real > 0.0 && weight_of(x) >= floor) {
                     first = (uint32_t)at;
                     weight = real;
                 }
@@ -1086,8 +1098,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
             const u64 rank = seen + __popcll(tied & ((1ull << lane) - 1));
             u64 y = 0;
             if (in && (k > cut || (k == cut && rank < ties))) {
-                const double real = w(x);
-                y = real >= least ? fixed(real) : 0;
+                y = kept_weight(x);
             }
             u64 upto = y;
             for (int d = 1; d < 64; d <<= 1) {
@@ -1135,7 +1146,7 @@ size_t sample_workspace_bytes(int64_t vocab, int64_t rows, int) {
 hipError_t launch_sample(const SampleArgs& a, asd_dtype dtype, void* workspace, int cus, hipStream_t stream) {
     int bits = 62;
     while (((int64_t)1 << (62 - bits)) < a.vocab) --bits;
-    if (bits > 52) bits = 52;
+    if (bits > 50) bits = 50;
     Stats s;
     s.groups = most_groups(a.vocab);
     const size_t groups = (size_t)s.groups * (size_t)a.rows;
