@@ -66,6 +66,22 @@ def test_long_blocks_and_many_requests():
     check_append(b, q, k, v, inv_freq=freq(64))
 
 
+@pytest.mark.parametrize("d", [16, 24])
+def test_more_requests_than_workgroups(d):
+    n, size = 70000, 4
+    k = torch.randn(n, 1, d, device=DEV).to(BF16)
+    v = torch.randn(n, 1, d, device=DEV).to(BF16)
+    pages = torch.randperm(n, device=DEV)
+    lens = torch.arange(n, device=DEV) % size
+    k_cache, v_cache = (torch.zeros(n, size, 1, d, dtype=BF16, device=DEV) for _ in range(2))
+    asd.asd_rope_append(None, k, v, k_cache, v_cache, pages.to(torch.int32)[:, None], lens,
+                        torch.zeros(n, dtype=torch.int32, device=DEV), None)
+    for cache, rows in ((k_cache, k), (v_cache, v)):
+        want = torch.zeros_like(cache)
+        want[pages, lens] = rows
+        assert torch.equal(cache, want)
+
+
 def test_offsets_leave_other_rows_as_they_were():
     b = Batch([2, 0, 3], [9, 4, 0], 4, 2, 64, BF16, 8, offsets=[10, 2, 5], total_rows=20)
     q, k, v = qkv(b)
