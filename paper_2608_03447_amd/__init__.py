@@ -26,8 +26,8 @@ from .build import BINDING, DECODE_HEADERS, DECODE_SOURCES, HASHED_SOURCES, LIBR
 __all__ = ["asd_verify", "asd_verify_static", "asd_verify_ws", "asd_verify_ex", "asd_shard_argmax",
            "asd_verify_partials", "asd_opportunity", "asd_commit", "asd_verify_commit",
            "asd_lmhead_verify", "asd_rope_append", "asd_block_attention", "asd_sample",
-           "asd_block_attention_workspace_bytes", "asd_sample_workspace_bytes", "asd_device_error", "asd_row_splits", "asd_row_pass", "asd_read_probe",
-           "asd_mfma_probe", "asd_workspace_bytes",
+           "asd_block_attention_workspace_bytes", "asd_sample_workspace_bytes", "asd_device_error",
+           "asd_row_splits", "asd_row_pass", "asd_read_probe", "asd_mfma_probe", "asd_workspace_bytes",
            "asd_status_string", "asd_version", "asd_release", "AsdError", "ASD_F32", "ASD_BF16", "ASD_F16",
            "ASD_GATE_RAW", "ASD_DEVERR_NEGATIVE_K", "ASD_DEVERR_ROWS", "ASD_DEVERR_COMMIT",
            "ASD_DEVERR_CACHE", "ASD_DEVERR_SAMPLE",
@@ -198,7 +198,10 @@ def _load_fast():
         verify_partials=bind(binding.verify_partials, "asd_verify_partials"),
         lmhead_verify=bind(binding.lmhead_verify, "asd_lmhead_verify"),
         shard_argmax=bind(binding.shard_argmax, "asd_shard_argmax"),
-        opportunity=bind(binding.opportunity, "asd_opportunity"))
+        opportunity=bind(binding.opportunity, "asd_opportunity"),
+        rope_append=bind(binding.rope_append, "asd_rope_append"),
+        block_attention=bind(binding.block_attention, "asd_block_attention"),
+        sample=bind(binding.sample, "asd_sample"))
     return _fast
 
 

@@ -26,6 +26,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+
 #include "../../include/asd.h"
 
 #ifndef ASD_BINDING_HASH
@@ -353,6 +355,247 @@ PyObject* opportunity(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
+// A strided GPU tensor on the current device with elements, or nullptr.
+const at::Tensor* strided(PyObject* o, int device) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.defined() || t.layout() != at::kStrided || !t.is_cuda() || !t.has_storage() ||
+        t.get_device() != device || t.numel() == 0)
+        return nullptr;
+    return &t;
+}
+
+bool half_type(const at::Tensor& t, asd_dtype* out) {
+    *out = t.scalar_type() == ScalarType::BFloat16 ? ASD_BF16 : ASD_F16;
+    return t.scalar_type() == ScalarType::BFloat16 || t.scalar_type() == ScalarType::Half;
+}
+
+// [rows, heads, D] in bf16 or f16 with the heads of a row dense; a type, rows or dim that are set already
+// are those it has to have.
+struct Heads {
+    const at::Tensor* t = nullptr;
+    void* ptr = nullptr;
+    int64_t stride = 0, heads = 0;
+    bool take(PyObject* o, int device, const at::Tensor* like) {
+        t = strided(o, device);
+        if (!t || t->dim() != 3) return false;
+        if (like && (t->scalar_type() != like->scalar_type() || t->size(0) != like->size(0) ||
+                     t->size(2) != like->size(2)))
+            return false;
+        heads = t->size(1);
+        const int64_t d = t->size(2);
+        if ((d > 1 && t->stride(2) != 1) || (heads > 1 && t->stride(1) != d) || heads > INT32_MAX ||
+            d > INT32_MAX)
+            return false;
+        stride = t->size(0) > 1 ? t->stride(0) : heads * d;
+        ptr = t->data_ptr();
+        return true;
+    }
+};
+
+// The batch and the cache of the decoding operators, from args[0]: key cache, value cache, page table,
+// cache lengths, block lengths, row offsets.
+constexpr int kPaged = 6;
+struct Paged {
+    asd_paged_cache cache;
+    int32_t n = 0;
+    void *cached, *lens, *offsets;
+    bool take(PyObject* const* a, int device, const at::Tensor& like) {
+        const at::Tensor *k = strided(a[0], device), *v = strided(a[1], device);
+        if (!k || !v || k->dim() != 4 || v->dim() != 4 || k->scalar_type() != like.scalar_type() ||
+            v->scalar_type() != like.scalar_type() || k->size(3) != like.size(2) ||
+            k->sizes() != v->sizes() || k->strides() != v->strides() ||
+            (k->size(3) > 1 && k->stride(3) != 1))
+            return false;
+        const at::Tensor* l = dense(a[4], ScalarType::Int, device);
+        const at::Tensor* table = dense(a[2], ScalarType::Int, device);
+        if (!l || l->dim() != 1 || l->size(0) > INT32_MAX || !table || table->dim() != 2 ||
+            table->size(0) != l->size(0) || table->size(1) > INT32_MAX || k->size(1) > INT32_MAX ||
+            k->size(2) > INT32_MAX || !vec(a[3], ScalarType::Long, l->size(0), device, &cached) ||
+            !vec(a[5], ScalarType::Long, l->size(0), device, &offsets, true))
+            return false;
+        n = (int32_t)l->size(0);
+        lens = l->data_ptr();
+        // a stride over one entry is never used; torch leaves it with any value
+        const auto step = [k](int i) { return k->size(i) > 1 ? k->stride(i) : 0; };
+        cache = {k->data_ptr(), v->data_ptr(), k->size(0), step(0), step(1), step(2),
+                 (const int32_t*)table->data_ptr(), (int32_t)table->size(1), (int32_t)k->size(1),
+                 (int32_t)k->size(2), (int32_t)k->size(3)};
+        return true;
+    }
+};
+
+// A caller's workspace, or None.
+bool space(PyObject* o, int device, void** ptr, size_t* bytes) {
+    *ptr = nullptr;
+    *bytes = 0;
+    if (o == Py_None) return true;
+    const at::Tensor* t = dense(o, ScalarType::Byte, device);
+    if (!t || t->numel() == 0) return false;
+    *ptr = t->data_ptr();
+    *bytes = (size_t)t->numel();
+    return true;
+}
+
+// An output that the caller gave (owned reference) or a fresh one.
+struct Output {
+    PyObject* given = nullptr;
+    at::Tensor fresh;
+    void* ptr = nullptr;
+    void keep(PyObject* o, void* p) {
+        Py_INCREF(o);
+        given = o;
+        ptr = p;
+    }
+    void make(at::IntArrayRef sizes, const at::TensorOptions& options) {
+        fresh = at::empty(sizes, options.requires_grad(false));
+        ptr = fresh.data_ptr();
+    }
+    PyObject* result(asd_status st) {
+        if (st != ASD_OK) return PyLong_FromLong(st);
+        if (!given) return THPVariable_Wrap(std::move(fresh));
+        Py_INCREF(given);
+        return given;
+    }
+    ~Output() { Py_XDECREF(given); }
+};
+
+// rope_append(entry, k, q, v, paged..., inv_freq, q_norm, k_norm, eps, positions, interleaved, out_q):
+// out_q, or True without q
+PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    constexpr int kRest = 4 + kPaged;
+    if (nargs != kRest + 7 || !PyFloat_CheckExact(a[kRest + 3]) || !PyBool_Check(a[kRest + 5]))
+        Py_RETURN_NONE;
+    const int device = current_device(a[1]);
+    Heads k, v, q, out;
+    Paged p;
+    asd_dtype dtype;
+    if (device < 0 || !k.take(a[1], device, nullptr) || !half_type(*k.t, &dtype) ||
+        !v.take(a[3], device, k.t) || v.heads != k.heads || !p.take(a + 4, device, *k.t) ||
+        p.cache.num_heads != k.heads)
+        Py_RETURN_NONE;
+    const int64_t rows = k.t->size(0), dim = k.t->size(2);
+    PyObject* const* r = a + kRest;
+    void *freq, *q_norm, *k_norm, *positions;
+    const ScalarType type = k.t->scalar_type();
+    if (!vec(r[0], ScalarType::Float, -1, device, &freq, true) ||
+        !vec(r[1], type, dim, device, &q_norm, true) || !vec(r[2], type, dim, device, &k_norm, true) ||
+        !vec(r[4], ScalarType::Long, rows, device, &positions, true))
+        Py_RETURN_NONE;
+    const int64_t rot = r[0] == Py_None ? 0 : 2 * THPVariable_Unpack(r[0]).numel();
+    if (rot > dim) Py_RETURN_NONE;
+    Output o;
+    if (a[2] == Py_None) {
+        if (r[6] != Py_None) Py_RETURN_NONE;
+    } else {
+        if (!q.take(a[2], device, k.t)) Py_RETURN_NONE;
+        if (r[6] == Py_None) {
+            o.make(q.t->sizes(), q.t->options());
+            out.stride = q.heads * dim;
+        } else {
+            if (!out.take(r[6], device, k.t) || out.heads != q.heads) Py_RETURN_NONE;
+            o.keep(r[6], out.ptr);
+        }
+    }
+    const float eps = (float)PyFloat_AS_DOUBLE(r[3]);
+    const uint32_t flags = r[5] == Py_True ? (uint32_t)ASD_ROPE_INTERLEAVED : 0u;
+    void* const stream = current_stream(device);
+    const auto f = entry<decltype(&asd_rope_append)>(a[0]);
+    const asd_status st = unlocked([&] {
+        return f(q.ptr, k.ptr, v.ptr, dtype, q.stride, k.stride, v.stride, (int32_t)q.heads, q_norm,
+                 k_norm, eps, (const float*)freq, (int32_t)rot, flags, (const int64_t*)positions,
+                 &p.cache, p.n, rows, (const int32_t*)p.lens, (const int64_t*)p.offsets,
+                 (const int64_t*)p.cached, o.ptr, out.stride, stream);
+    });
+    return a[2] == Py_None ? done(st) : o.result(st);
+    END_HANDLE_TH_ERRORS
+}
+
+// block_attention(entry, q, paged..., scale, mask, out, workspace)
+PyObject* block_attention(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    constexpr int kRest = 2 + kPaged;
+    if (nargs != kRest + 4) Py_RETURN_NONE;
+    const int device = current_device(a[1]);
+    Heads q;
+    Paged p;
+    asd_dtype dtype;
+    if (device < 0 || !q.take(a[1], device, nullptr) || !half_type(*q.t, &dtype) ||
+        !p.take(a + 2, device, *q.t))
+        Py_RETURN_NONE;
+    const int64_t rows = q.t->size(0), dim = q.t->size(2);
+    PyObject* const* r = a + kRest;
+    void *mask = nullptr, *ws;
+    int32_t words = 0;
+    size_t ws_bytes;
+    if (r[0] != Py_None && !PyFloat_CheckExact(r[0])) Py_RETURN_NONE;
+    const float scale =
+        (float)(r[0] == Py_None ? 1.0 / std::sqrt((double)dim) : PyFloat_AS_DOUBLE(r[0]));
+    if (r[1] != Py_None) {
+        const at::Tensor* m = dense(r[1], ScalarType::Long, device);
+        if (!m || m->dim() != 2 || m->size(0) != rows || m->size(1) < 1 || m->size(1) > INT32_MAX)
+            Py_RETURN_NONE;
+        mask = m->data_ptr();
+        words = (int32_t)m->size(1);
+    }
+    Output o;
+    if (r[2] == Py_None) {
+        o.make(q.t->sizes(), q.t->options());
+    } else {
+        const at::Tensor* t = dense(r[2], q.t->scalar_type(), device);
+        if (!t || t->sizes() != q.t->sizes()) Py_RETURN_NONE;
+        o.keep(r[2], t->data_ptr());
+    }
+    if (!space(r[3], device, &ws, &ws_bytes)) Py_RETURN_NONE;
+    void* const stream = current_stream(device);
+    const auto f = entry<decltype(&asd_block_attention)>(a[0]);
+    return o.result(unlocked([&] {
+        return f(q.ptr, dtype, q.stride, (int32_t)q.heads, scale, &p.cache, p.n, rows,
+                 (const int32_t*)p.lens, (const int64_t*)p.offsets, (const int64_t*)p.cached,
+                 (const uint64_t*)mask, words, o.ptr, stream, ws, ws_bytes);
+    }));
+    END_HANDLE_TH_ERRORS
+}
+
+// sample(entry, logits, uniform, temperature, top_k, top_p, min_p, out_token, out_prob, workspace)
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    if (nargs != 10) Py_RETURN_NONE;
+    const int device = current_device(a[1]);
+    const at::Tensor* z = device < 0 ? nullptr : strided(a[1], device);
+    if (!z || z->dim() != 2) Py_RETURN_NONE;
+    asd_dtype dtype = ASD_F32;
+    if (z->scalar_type() != ScalarType::Float && !half_type(*z, &dtype)) Py_RETURN_NONE;
+    const int64_t rows = z->size(0), vocab = z->size(1), stride = rows > 1 ? z->stride(0) : vocab;
+    void *uniform, *temperature, *top_k, *top_p, *min_p, *prob, *token, *ws;
+    size_t ws_bytes;
+    if ((vocab > 1 && z->stride(1) != 1) || stride < vocab ||
+        !vec(a[2], ScalarType::Float, rows, device, &uniform) ||
+        !vec(a[3], ScalarType::Float, rows, device, &temperature, true) ||
+        !vec(a[4], ScalarType::Int, rows, device, &top_k, true) ||
+        !vec(a[5], ScalarType::Float, rows, device, &top_p, true) ||
+        !vec(a[6], ScalarType::Float, rows, device, &min_p, true) ||
+        !vec(a[7], ScalarType::Int, rows, device, &token, true) ||
+        !vec(a[8], ScalarType::Float, rows, device, &prob, true) ||
+        !space(a[9], device, &ws, &ws_bytes))
+        Py_RETURN_NONE;
+    Output o;
+    if (a[7] != Py_None)
+        o.keep(a[7], token);
+    else
+        o.make({rows}, z->options().dtype(ScalarType::Int));
+    const void* const ptr = z->data_ptr();
+    void* const stream = current_stream(device);
+    const auto f = entry<decltype(&asd_sample)>(a[0]);
+    return o.result(unlocked([&] {
+        return f(ptr, dtype, vocab, rows, stride, (const float*)temperature, (const int32_t*)top_k,
+                 (const float*)top_p, (const float*)min_p, (const float*)uniform, (int32_t*)o.ptr,
+                 (float*)prob, stream, ws, ws_bytes);
+    }));
+    END_HANDLE_TH_ERRORS
+}
+
 PyObject* source_hash(PyObject*, PyObject*) { return PyUnicode_FromString(ASD_BINDING_HASH); }
 
 #define ASD_FAST(name) \
@@ -360,7 +603,9 @@ PyObject* source_hash(PyObject*, PyObject*) { return PyUnicode_FromString(ASD_BI
 PyMethodDef methods[] = {ASD_FAST(verify),        ASD_FAST(verify_ex),
                          ASD_FAST(verify_commit), ASD_FAST(verify_partials),
                          ASD_FAST(lmhead_verify), ASD_FAST(shard_argmax),
-                         ASD_FAST(opportunity),   {"source_hash", source_hash, METH_NOARGS, nullptr},
+                         ASD_FAST(opportunity),   ASD_FAST(rope_append),
+                         ASD_FAST(block_attention), ASD_FAST(sample),
+                         {"source_hash", source_hash, METH_NOARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_asd_binding", nullptr, -1, methods};

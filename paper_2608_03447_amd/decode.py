@@ -3,7 +3,8 @@ the paged cache (``asd_rope_append``), its rows attend to the cache
 (``asd_block_attention``), and tokens are drawn from logit rows (``asd_sample``).
 
 Like the rest of the binding these only marshal torch tensors and the current
-HIP stream into the C calls of ``include/asd.h``.
+HIP stream into the C calls of ``include/asd.h``, the ordinary arguments in
+``_asd_binding``.
 """
 import ctypes
 import math
@@ -109,6 +110,11 @@ def asd_rope_append(q, k, v, k_cache, v_cache, page_table, cache_lens, block_len
     Returns the rotated queries (None without q); the cache is written in place.  Rows that no
     request owns are not written.
     """
+    r = (_asd._fast or _asd._load_fast()).rope_append(
+        k, q, v, k_cache, v_cache, page_table, cache_lens, block_lens, row_offsets, inv_freq, q_norm,
+        k_norm, eps, positions, interleaved, out_q)
+    if r is not None:
+        return None if r is True else _asd._result(r, "asd_rope_append")
     if k.dim() != 3 or not k.is_cuda or k.dtype not in _HALF:
         raise ValueError("k must be a 3-D bfloat16 or float16 tensor [rows, heads, D] on a GPU")
     dev, dtype = k.device, k.dtype
@@ -165,6 +171,11 @@ def asd_block_attention(q, k_cache, v_cache, page_table, cache_lens, block_lens,
     workspace    None (library workspace) or a uint8 tensor as for :func:`asd_verify_ws`
     Returns out, [total_rows, q_heads, D]; rows that no request owns are not written.
     """
+    r = (_asd._fast or _asd._load_fast()).block_attention(
+        q, k_cache, v_cache, page_table, cache_lens, block_lens, row_offsets, scale, mask, out,
+        workspace)
+    if r is not None:
+        return _asd._result(r, "asd_block_attention")
     stride = _heads(q, "q")
     dev, dtype = q.device, q.dtype
     rows, q_heads, dim = q.shape
@@ -213,6 +224,10 @@ def asd_sample(logits, uniform, *, temperature=None, top_k=None, top_p=None, min
     workspace    None (library workspace) or a uint8 tensor as for :func:`asd_verify_ws`
     Returns the tokens, int32 [rows].
     """
+    r = (_asd._fast or _asd._load_fast()).sample(
+        logits, uniform, temperature, top_k, top_p, min_p, out_token, out_prob, workspace)
+    if r is not None:
+        return _asd._result(r, "asd_sample")
     if logits.dim() != 2 or logits.dtype not in _DTYPES or not logits.is_cuda:
         raise ValueError("logits must be a 2-D float32, bfloat16 or float16 tensor on a GPU")
     rows, vocab = logits.shape
