@@ -338,13 +338,14 @@ template <int kN> struct Block {
         return all;
     }
     // Sums with one barrier: of a number that each wavefront has, and of one that each thread has.  The
-    // place alternates, so that a wavefront that is ahead does not write what another still reads.
-    uint32_t votes_of[2][kWaves];
+    // place alternates with `turn`, which the caller counts up, so that a wavefront that is ahead does not
+    // write what another still reads.
+    u64 votes_of[2][kWaves];
     double masses_of[2][kWaves];
-    __device__ __forceinline__ uint32_t votes(uint32_t of_wave, int turn) {
+    __device__ __forceinline__ u64 votes(u64 of_wave, int turn) {
         if ((threadIdx.x & 63) == 0) votes_of[turn & 1][threadIdx.x >> 6] = of_wave;
         __syncthreads();
-        uint32_t sum = 0;
+        u64 sum = 0;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) sum += votes_of[turn & 1][w];
         return sum;
@@ -420,7 +421,7 @@ __device__ __forceinline__ float inside_unit(float u) {
 
 // ------------------------------------------------------------ pass 2
 
-constexpr int kPickThreads = 256, kListed = 2048, kHeld = 16;
+constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64, kListed = 2048, kHeld = 8;
 constexpr int kMostSubs = kPickThreads * kHeld;          // sub-block maxima held in registers
 constexpr int kFewest = 192;                             // sub-blocks that candidates come from without top-k
 constexpr int kRanked = 2;                               // candidates a thread ranks by comparing each with each
@@ -435,7 +436,11 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     __shared__ Block<kPickThreads> block;
     __shared__ uint32_t key[kListed], place[kListed];
     __shared__ double weight[kListed];
-    __shared__ int32_t wanted[kMostSubs / 2];
+    __shared__ union {
+        int32_t wanted[kMostSubs / 2];                       // the sub-blocks to read, then
+        double ranked[kRanked * kPickThreads];               // the weights in order
+    } share;
+    int32_t* const wanted = share.wanted;
     __shared__ uint32_t starts[kMostSubs / 2 * (kSub / kPer) / 64];
     __shared__ int32_t found;
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_of_block();
@@ -528,35 +533,52 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     uint32_t held[kHeld];
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) held[i] = i * kPickThreads + tid < subs ? sub[i * kPickThreads + tid] : 0;
-    uint32_t least = 0;         // by bisection over its upper 16 bits
-    for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t trial = least | 1u << bit;
-        if (trial > top) continue;
-        uint32_t n = 0;
+    int turn = 0;               // of the sums with one barrier
+    uint32_t least = 0;         // by its upper 16 bits, two at a time
+    for (int bit = 30; bit >= 16; bit -= 2) {
+        if ((least | 1u << bit) > top) continue;
+        u64 n = 0;              // how many reach each of the three trials
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) {
             if (i * kPickThreads >= subs) break;
-            n += (uint32_t)__popcll(__ballot(held[i] >= trial));
+#pragma unroll
+            for (uint32_t c = 1; c < 4; ++c)
+                n += (u64)__popcll(__ballot(held[i] >= (least | c << bit))) << (20 * (c - 1));
         }
-        if (block.votes(n, bit) >= (uint32_t)need) least = trial;
+        n = block.votes(n, turn++);
+        for (uint32_t c = 3; c > 0; --c)
+            if ((uint32_t)(n >> (20 * (c - 1)) & 0xfffff) >= (uint32_t)need) {
+                least |= c << bit;
+                break;
+            }
     }
     least = max(least, kKeyNegInf);
-    // the sub-blocks that reach it, in order
-    int32_t blocks = 0;
+    // the sub-blocks that reach it, in order: the counts of each held[i] of each wavefront, summed up
+    static_assert(kHeld * kPickWaves == 64, "a lane a count");
+    uint32_t* const counts = starts;
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-        if (i * kPickThreads >= subs) break;
-        const bool in = held[i] >= least;
-        int32_t total;
-        const int32_t at = blocks + block.before((int32_t)in, (int32_t*)block.u, &total);
-        if (in && at < kMostSubs / 2) wanted[at] = i * kPickThreads + tid;
-        blocks += total;
+        const int c = __popcll(__ballot(held[i] >= least));
+        if (lane == 0) counts[i * kPickWaves + wave] = c;
+    }
+    __syncthreads();
+    int32_t upto = (int32_t)counts[lane];
+    for (int x = 1; x < 64; x <<= 1) {
+        const int32_t up = __shfl_up(upto, x);
+        if (lane >= x) upto += up;
+    }
+    const int32_t blocks = __shfl(upto, 63);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+        const u64 in = __ballot(held[i] >= least);
+        const int32_t at = __shfl(upto, i * kPickWaves + wave) - __popcll(in >> lane);
+        if (held[i] >= least && at < kMostSubs / 2) wanted[at] = i * kPickThreads + tid;
     }
     __syncthreads();
     // Their tokens, in order: a sweep that counts them, 64 vectors at a time, and one that lists them (the
     // second finds them in the L2); several loads of a wavefront are on the way at once.
     int32_t n = 0;
-    constexpr int kLanes = kSub / kPer, kAhead = 4, kWaves = kPickThreads / 64;
+    constexpr int kLanes = kSub / kPer, kAhead = 8, kWaves = kPickWaves;
     const int32_t sweeps = (blocks * kLanes + 63) / 64;
     if (blocks <= kMostSubs / 2) {
         const auto sweep = [&](auto&& f) {
@@ -627,42 +649,56 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
 
     const int each = (n + kPickThreads - 1) / kPickThreads, from = min(n, tid * each), to = min(n, from + each);
     if (n <= kRanked * kPickThreads) {
-        // Few: a candidate's rank, and the weight of those ranked before it, by comparing it with each.
-        uint32_t own[kRanked], rank[kRanked];
-        double before[kRanked];
-#pragma unroll
-        for (int c = 0; c < kRanked; ++c) {
-            const int i = c * kPickThreads + tid;
-            own[c] = i < n ? key[i] : 0;
-            rank[c] = 0;
-            before[c] = 0.0;
-        }
-#pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const uint32_t k = key[i];
-            const double x = weight[i];
+        // Few: a candidate's rank by comparing its key with each, a compare and an addition with carry; the
+        // weights before it by a sum over the weights in that order.
+        uint32_t rank[kRanked];
+        if (r.by_count || r.by_mass) {
+            if (tid < 64 && n + tid < (n + 63 & ~63)) key[n + tid] = 0;
+            for (int i = tid; i < kRanked * kPickThreads; i += kPickThreads) share.ranked[i] = 0.0;
+            __syncthreads();
 #pragma unroll
             for (int c = 0; c < kRanked; ++c) {
-                const bool first = k > own[c] || (k == own[c] && i < c * kPickThreads + tid);
-                rank[c] += first;
-                before[c] += first ? x : 0.0;
+                rank[c] = 0;
+                const int base = c * kPickThreads + wave * 64;
+                if (base >= n) break;
+                const uint32_t own = key[base + lane];
+                for (int j0 = 0; j0 < n; j0 += 64) {
+                    // of equal keys the earlier ranks first: those before this one count from its own key on
+                    const uint32_t bound = j0 < base ? own - 1 : own;
+                    if (j0 != base) {
+#pragma unroll 16
+                        for (int j = 0; j < 64; ++j) rank[c] += key[j0 + j] > bound;
+                    } else {
+#pragma unroll 16
+                        for (int j = 0; j < 64; ++j) rank[c] += key[j0 + j] > (j < lane ? own - 1 : own);
+                    }
+                }
+                if (base + lane < n && (!r.by_count || rank[c] < (uint32_t)r.k))
+                    share.ranked[rank[c]] = weight[base + lane];
+            }
+            __syncthreads();
+            if (r.by_mass) {
+                double of[kRanked], mine = 0.0, whole;
+#pragma unroll
+                for (int c = 0; c < kRanked; ++c) mine += of[c] = share.ranked[tid * kRanked + c];
+                double before = block.before(mine, block.d, &whole);
+                if (r.by_count) all = whole;
+#pragma unroll
+                for (int c = 0; c < kRanked; ++c) {
+                    share.ranked[tid * kRanked + c] = before;
+                    before += of[c];
+                }
+                __syncthreads();
             }
         }
-        double kept[kRanked], mine = 0.0;
-#pragma unroll
-        for (int c = 0; c < kRanked; ++c) {
-            const int i = c * kPickThreads + tid;
-            kept[c] = i < n && (!r.by_count || rank[c] < (uint32_t)r.k) ? weight[i] : 0.0;
-            mine += kept[c];
-        }
-        if (r.by_count) all = block.sum(mine);
         const double goal = (double)r.p * all;
-        __syncthreads();
 #pragma unroll
         for (int c = 0; c < kRanked; ++c) {
             const int i = c * kPickThreads + tid;
-            if (i < n)
-                weight[i] = kept[c] >= floor && (!r.by_mass || rank[c] == 0 || before[c] < goal) ? kept[c] : 0.0;
+            if (i >= n) break;
+            if (weight[i] < floor || (r.by_count && rank[c] >= (uint32_t)r.k) ||
+                (r.by_mass && rank[c] != 0 && !(share.ranked[rank[c]] < goal)))
+                weight[i] = 0.0;
         }
     } else {
         // The greatest key that enough tokens, or tokens of enough weight, reach, bit by bit from the first
@@ -670,17 +706,17 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
         const int first_bit = top == least ? -1 : 31 - __builtin_clz(top ^ least);
         const uint32_t common = first_bit == 31 ? 0u : top & ~((2u << max(first_bit, 0)) - 1u);
         const uint32_t start = first_bit < 0 ? top : common;
-        const auto above = [&](uint32_t bound, int turn) {          // weight of the keys greater than it
+        const auto above = [&](uint32_t bound) {          // weight of the keys greater than it
             double x = 0.0;
             for (int i = tid; i < n; i += kPickThreads)
                 if (key[i] > bound) x += weight[i];
-            return block.mass(x, turn);
+            return block.mass(x, turn++);
         };
-        const auto reaching = [&](uint32_t bound, int turn) {       // tokens whose keys reach it
+        const auto reaching = [&](uint32_t bound) {       // tokens whose keys reach it
             uint32_t c = 0;
             for (int i = 0; i < n; i += kPickThreads)
                 c += (uint32_t)__popcll(__ballot(i + tid < n && key[i + tid] >= bound));
-            return block.votes(c, turn);
+            return (uint32_t)block.votes(c, turn++);
         };
         uint32_t cut = 0;
         int32_t ties = 0x7fffffff;
@@ -688,22 +724,22 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
         if (r.by_count) {
             cut = start;
             for (int bit = first_bit; bit >= 0; --bit)
-                if (reaching(cut | 1u << bit, bit) >= (uint32_t)r.k) cut |= 1u << bit;
-            const int32_t more = (int32_t)reaching(cut + 1, 1);
+                if (reaching(cut | 1u << bit) >= (uint32_t)r.k) cut |= 1u << bit;
+            const int32_t more = (int32_t)reaching(cut + 1);
             ties = r.k - more;
             const double one = w(value_of(cut));
-            beyond = ((int32_t)reaching(cut, 0) - r.k) * one;
-            all = above(cut, 0) + ties * one;
+            beyond = ((int32_t)reaching(cut) - r.k) * one;
+            all = above(cut) + ties * one;
         }
         if (r.by_mass && (r.by_count || sum >= (double)r.p * all)) {
             const double goal = (double)r.p * all;
             uint32_t t = start;
             for (int bit = first_bit; bit >= 0; --bit) {
                 const uint32_t trial = t | 1u << bit;
-                const double reach = above(trial - 1, bit) - (trial <= cut ? beyond : 0.0);
+                const double reach = above(trial - 1) - (trial <= cut ? beyond : 0.0);
                 if (reach >= goal && reach > 0.0) t = trial;
             }
-            const double one = w(value_of(t)), missing = goal - above(t, 1);
+            const double one = w(value_of(t)), missing = goal - above(t);
             const int32_t m = max(1, one > 0.0 ? (int32_t)min(ceil(missing / one), 2e9) : 1);
             ties = t == cut ? min(ties, m) : m;
             cut = t;
