@@ -107,13 +107,33 @@ struct Row {
     }
 };
 
+// Who draws a row's token: pass 2, one workgroup of pass 5, or passes 3 and 4, and pass 5 from what they leave.
+enum { kDone = 0, kAlone = 1, kShared = 2 };
+
+// A shared row's bins: of one width in the logit, counted up to the last one, which all from `high` on are in.
+constexpr int kNearBins = 1024;
+struct Near {
+    float high, steps;     // steps: bins to a unit of the logit
+    uint32_t top;          // key of the greatest logit
+    uint32_t collected;    // tokens of the cut's bin that pass 4 listed, in the place of the row's sub-blocks
+    u64 rest;              // mass that is wanted of them
+    __device__ __forceinline__ uint32_t bin(float x) const {
+        return (uint32_t)(kNearBins - 1) - (uint32_t)fminf(fmaxf((high - x) * steps, 0.0f), (float)(kNearBins - 1));
+    }
+};
+
 // What pass 1 leaves of a row: keys of its sub-blocks' maxima, keys and sums of its groups.
 struct Stats {
     uint32_t* subs;        // [rows][groups * kSubs]
     uint32_t* tops;        // [rows][groups]
     double* sums;          // [rows][groups]
-    int32_t* flat;         // [rows]: 1: left to pass 3
+    int32_t* flat;         // [rows]: kDone, or who has the row next
     int32_t groups;        // of the row that has most: its first vector may begin before it
+    // where rows are shared out (shares_out(vocab)), else null:
+    uint32_t* queued;      // how many such rows,
+    int32_t* queue;        // [rows] and which
+    Near* near;            // [rows]
+    u64* bins;             // [rows][kNearBins]: weights by their bin
 };
 
 // A row as 16-byte vectors: its elements stand `shift` places behind the vector grid's origin.
@@ -211,6 +231,7 @@ __global__ __launch_bounds__(kScanThreads) void asd_sample_scan_kernel(SampleArg
     const int lane = threadIdx.x & 63, wave = wave_of_block();
     const int64_t row = blockIdx.x / tiles;
     const int32_t tile = (int32_t)(blockIdx.x - row * tiles);
+    if (s.queued && blockIdx.x == 0 && threadIdx.x == 0) *s.queued = 0;
     const Grid<T> z(a, row);
     const Row r(a, row);
     const bool whole = !r.greedy && !r.by_count;
@@ -455,7 +476,7 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
         a.out_token[row] = at < 0 ? -1 : (int32_t)(at - z.shift);
         if (a.out_prob) a.out_prob[row] = (float)prob;
     };
-    if (tid == 0) s.flat[row] = 0;
+    if (tid == 0) s.flat[row] = kDone;
 
     uint32_t top = 0;
     for (int32_t g = tid; g < groups; g += kPickThreads) top = max(top, tops[g]);
@@ -527,7 +548,7 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     // Candidates: every token whose key reaches `least`, which `need` sub-blocks' maxima do.
     const int32_t need = r.by_count ? r.k : max(1, min(kFewest, subs / 2));
     if (subs > kMostSubs || (r.by_count && r.k > most_k(subs))) {
-        if (tid == 0) s.flat[row] = 1;
+        if (tid == 0) s.flat[row] = kAlone;
         return;
     }
     uint32_t held[kHeld];
@@ -633,8 +654,28 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
                     }
             });
     }
+    // What is left to the passes over whole rows.  The mass is reached below `least` as a rule, so the bins of a
+    // shared row begin there; they reach four times as far as the lowest sub-block's maximum, which in rows of
+    // any spread leaves 1 in 300 tokens or fewer in a bin.
+    const auto leave = [&] {
+        const bool shared = s.queued && !r.by_count && top < kKeyInf;
+        if (shared) {
+            uint32_t low = kKeyNan;
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i)
+                if (held[i] > kKeyNegInf) low = min(low, held[i]);
+            low = block.min(low);
+            for (int b = tid; b < kNearBins; b += kPickThreads) s.bins[row * kNearBins + b] = 0;
+            if (tid == 0) {
+                const float high = value_of(least), range = 4.0f * (high - value_of(low));
+                s.near[row] = Near{high, range > 0.0f ? kNearBins / range : 0.0f, top, 0, 0};
+                s.queue[atomicAdd(s.queued, 1u)] = (int32_t)row;
+            }
+        }
+        if (tid == 0) s.flat[row] = shared ? kShared : kAlone;
+    };
     if (blocks > kMostSubs / 2 || n > kListed) {
-        if (tid == 0) s.flat[row] = 1;
+        leave();
         return;
     }
     __syncthreads();
@@ -643,7 +684,7 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     const double floor = r.by_floor ? (double)r.m : 0.0, sum = block.sum(mine);
     if (!r.by_count && least != kKeyNegInf &&            // some tokens are no candidates
         !(r.by_mass && sum >= (double)r.p * all) && !(r.by_floor && w(value_of(least)) < floor)) {
-        if (tid == 0) s.flat[row] = 1;
+        leave();
         return;
     }
 
@@ -774,9 +815,7 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     }
 }
 
-// ------------------------------------------------------------ pass 3
-
-constexpr int kFlatThreads = 1024, kFlatWaves = kFlatThreads / 64, kBins = 4096, kCollected = 8192, kSpans = 1024;
+// ------------------------------------------------------------ whole rows
 
 // ceil and floor of f * total for a float 0 <= f < 1 and an integer below 2^63, exactly.
 __device__ __forceinline__ u64 share(float f, u64 total, bool up) {
@@ -789,12 +828,171 @@ __device__ __forceinline__ u64 share(float f, u64 total, bool up) {
     return (u64)((x + (up ? ((unsigned __int128)1 << shift) - 1 : 0)) >> shift);
 }
 
+// Weights as whole numbers of 2^-bits of the greatest, so that their sum is the same in any order: added to
+// 2^(52 - bits) a weight is rounded to one, which then stands in the sum's low bits.  (A weight below half a
+// unit gives 0, as -inf does.)
+struct Units {
+    Weights w;
+    double carrier;
+    bool finite;                    // the greatest logit: then no token needs care
+    __device__ __forceinline__ Units(const Weights& w, int bits, uint32_t top)
+        : w(w), carrier((double)(1ull << (52 - bits))), finite(top < kKeyInf) {}
+    __device__ __forceinline__ u64 operator()(float z) const {
+        const double x = finite ? power2_clamped(((double)z - w.top) * w.per) : w(z);
+        return __builtin_bit_cast(u64, x + carrier) - __builtin_bit_cast(u64, carrier);
+    }
+};
+
+// Calls f(value, grid place) for every token of the row's groups g, g + step, ... below `stop`, by one
+// wavefront; a group's end is told by end(group).
+template <typename T, typename F, typename E>
+__device__ __forceinline__ void over_groups(const Grid<T>& z, int32_t g, int32_t stop, int32_t step, F&& f, E&& end) {
+    constexpr int kPer = 16 / sizeof(T), kLoads = kGroup / (64 * kPer);
+    const int lane = threadIdx.x & 63;
+    const int32_t groups = z.groups();
+    if (g >= stop) return;
+    u32x4 next[kLoads];
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) next[l] = load_vector(z, (int64_t)g * kGroup + (l * 64 + lane) * kPer);
+    for (; g < stop; g += step) {
+        u32x4 raw[kLoads];
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) raw[l] = next[l];
+        if (g + step < stop) {
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l)
+                next[l] = load_vector(z, (int64_t)(g + step) * kGroup + (l * 64 + lane) * kPer);
+        }
+        const bool edge = g == 0 || g + 1 >= groups;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            float x[kPer];
+            unpack<T>(raw[l], x);
+            const int64_t at = (int64_t)g * kGroup + (l * 64 + lane) * kPer;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (!edge || z.has(at + e)) f(x[e], at + e);
+        }
+        end(g);
+    }
+}
+
+// ------------------------------------------------------------ passes 3 and 4
+
+// Rows that keep more tokens than pass 2 holds, by mass alone: every row in parts, all workgroups of the launch
+// taking parts in turn.  Pass 3 sums the weights by bins of the logit.  Pass 4 finds the bin in which the mass
+// is reached, sums each group's weights above it and lists the bin's own tokens.
+constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPartList = 1024;
+
+// Vocabularies whose rows are shared out: sub-blocks that pass 2 can hold, and rows long enough for two more
+// launches.  One workgroup took 220 us for a row of 129,280.
+bool shares_out(int64_t vocab) { return vocab > 65536 && vocab + 7 <= (int64_t)kMostSubs * kSub; }
+
+// Shared tokens of a row that its list has room for, in the place of its sub-blocks' maxima.
+__device__ __forceinline__ uint32_t list_room(const Stats& s) { return (uint32_t)s.groups * (kSubs / 2); }
+
+template <int kType, bool kSurvey>
+__global__ __launch_bounds__(kPartThreads) void asd_sample_part_kernel(SampleArgs a, Stats s, int bits) {
+    typedef typename Element<kType>::T T;
+    __shared__ Block<kPartThreads> block;
+    __shared__ u64 box[kSurvey ? kPartList : kNearBins];      // listed tokens, or the part's bins
+    __shared__ u64 found[2];
+    __shared__ uint32_t listed, start;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_of_block();
+    const uint32_t rows = *s.queued;
+    if (rows == 0) return;
+    // parts of 4 groups at least, and two to a workgroup where there are enough
+    const uint32_t parts = max(1u, min((2 * gridDim.x + rows - 1) / rows, (uint32_t)s.groups / kPartWaves));
+    for (int64_t unit = blockIdx.x; unit < (int64_t)rows * parts; unit += gridDim.x) {
+        const int64_t row = s.queue[unit / parts];
+        const uint32_t part = (uint32_t)(unit % parts);
+        const Grid<T> z(a, row);
+        const Row r(a, row);
+        if (!kSurvey && !r.by_mass) continue;        // min-p alone: no bin to find
+        Near* const mine = s.near + row;
+        const Near near{mine->high, mine->steps, mine->top, 0, 0};
+        u64* const bins = s.bins + row * kNearBins;
+        const Units weight_of(Weights(value_of(near.top), r.t), bits, near.top);
+        const int64_t groups = z.groups();
+        const int32_t from = (int32_t)(part * groups / parts), to = (int32_t)((part + 1) * groups / parts);
+        if constexpr (!kSurvey) {
+            for (int b = tid; b < kNearBins; b += kPartThreads) box[b] = 0;
+            __syncthreads();
+            over_groups(
+                z, from + wave, to, kPartWaves, [&](float x, int64_t) { atomicAdd(&box[near.bin(x)], weight_of(x)); },
+                [](int32_t) {});
+            __syncthreads();
+            for (int b = tid; b < kNearBins; b += kPartThreads)
+                if (box[b] != 0) atomicAdd(&bins[b], box[b]);
+            __syncthreads();
+        } else {
+            if (tid == 0) listed = 0;
+            int32_t bin = -1;            // of the cut: without one all tokens are above
+            if (r.by_mass) {
+                // from the last bin down
+                constexpr int kEach = kNearBins / kPartThreads;
+                u64 each[kEach], sum = 0, total;
+#pragma unroll
+                for (int c = 0; c < kEach; ++c) sum += each[c] = bins[kNearBins - 1 - (tid * kEach + c)];
+                u64 have = block.before(sum, block.u, &total);
+                const u64 want = max((u64)1, share(r.p, total, true));
+                if (have < want && have + sum >= want) {
+#pragma unroll
+                    for (int c = 0; c < kEach; ++c) {
+                        if (have < want && have + each[c] >= want) {
+                            found[0] = (u64)(kNearBins - 1 - (tid * kEach + c));
+                            found[1] = want - have;
+                        }
+                        have += each[c];
+                    }
+                }
+                __syncthreads();
+                bin = (int32_t)found[0];
+                if (part == 0 && tid == 0) mine->rest = found[1];
+            } else {
+                __syncthreads();
+            }
+            const u64 floor = r.by_floor ? (u64)ceil((double)r.m * (double)(1ull << bits)) : 0;
+            u64 above = 0;
+            over_groups(
+                z, from + wave, to, kPartWaves,
+                [&](float x, int64_t at) {
+                    const int32_t b = (int32_t)near.bin(x);
+                    if (b > bin) {
+                        const u64 y = weight_of(x);
+                        above += y >= floor ? y : 0;
+                    } else if (b == bin) {
+                        const uint32_t i = atomicAdd(&listed, 1u);
+                        if (i < kPartList) box[i] = (u64)at << 32 | key_of(x);
+                    }
+                },
+                [&](int32_t g) {
+                    for (int x = 32; x > 0; x >>= 1) above += (u64)__shfl_xor((long long)above, x);
+                    if (lane == 0) ((u64*)s.sums)[row * s.groups + g] = above;
+                    above = 0;
+                });
+            __syncthreads();
+            // more than there is room for: a number that no list has
+            if (tid == 0 && listed > 0) start = atomicAdd(&mine->collected, listed <= kPartList ? listed : 1u << 24);
+            __syncthreads();
+            const uint32_t n = min(listed, (uint32_t)kPartList);
+            u64* const list = (u64*)(s.subs + row * s.groups * kSubs);
+            for (uint32_t i = tid; i < n; i += kPartThreads)
+                if (start + i < list_room(s)) list[start + i] = box[i];
+            __syncthreads();
+        }
+    }
+}
+
+// ------------------------------------------------------------ pass 5
+
+constexpr int kFlatThreads = 1024, kFlatWaves = kFlatThreads / 64, kBins = 4096, kCollected = 8192, kSpans = 1024;
+
 // A workgroup a row.  Weights are whole numbers of 2^-bits of the greatest, so that sums over any order are
 // the same; spans of `span` tokens (1,024 up to 2^20 tokens a row) hold what is kept of them.
 template <int kType>
 __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArgs a, Stats s, int bits) {
     typedef typename Element<kType>::T T;
-    constexpr int kPer = 16 / sizeof(T);
     __shared__ Block<kFlatThreads> block;
     __shared__ u64 bin_weight[kBins];
     __shared__ uint32_t bin_count[kBins];
@@ -805,7 +1003,8 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
     __shared__ u64 pick[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_of_block();
     const int64_t row = blockIdx.x;
-    if (s.flat[row] == 0) return;
+    const int32_t state = s.flat[row];
+    if (state == kDone) return;
     const Grid<T> z(a, row);
     const Row r(a, row);
     const int32_t groups = z.groups(), per_span = (groups + kSpans - 1) / kSpans;
@@ -815,14 +1014,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
     top = block.max(top);
     const Weights w(value_of(top), r.t);
     const double unit = (double)(1ull << bits);
-    // A weight as a whole number of units: added to 2^(52 - bits) it is rounded to one, which then stands in the
-    // sum's low bits.  (A weight below half a unit gives 0, as -inf does.)
-    const double carrier = (double)(1ull << (52 - bits));
-    const auto fixed = [&](double x) { return __builtin_bit_cast(u64, x + carrier) - __builtin_bit_cast(u64, carrier); };
-    const bool finite = top < kKeyInf;          // the greatest logit: then no token needs care
-    const auto weight_of = [&](float z) -> u64 {
-        return fixed(finite ? power2_clamped(((double)z - w.top) * w.per) : w(z));
-    };
+    const Units weight_of(w, bits, top);
     // min-p in units: a weight counts from there on.  (Rounded up; the greatest token's always does.)
     const u64 floor = r.by_floor ? (u64)ceil((double)r.m * unit) : 0;
     const auto kept_weight = [&](float z) -> u64 {
@@ -830,33 +1022,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
         return x >= floor ? x : 0;
     };
 
-    // Calls f(value, grid place) for every token of the row, group by group, a wavefront each; a group's
-    // end is told by end(group).
-    const auto over = [&](auto&& f, auto&& end) {
-        constexpr int kLoads = kGroup / (64 * kPer);
-        u32x4 next[kLoads];
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) next[l] = load_vector(z, (int64_t)wave * kGroup + (l * 64 + lane) * kPer);
-        for (int32_t g = wave; g < groups; g += kFlatWaves) {
-            u32x4 raw[kLoads];
-#pragma unroll
-            for (int l = 0; l < kLoads; ++l) {
-                raw[l] = next[l];
-                next[l] = load_vector(z, (int64_t)(g + kFlatWaves) * kGroup + (l * 64 + lane) * kPer);
-            }
-            const bool edge = g == 0 || g + 1 >= groups;
-#pragma unroll
-            for (int l = 0; l < kLoads; ++l) {
-                float x[kPer];
-                unpack<T>(raw[l], x);
-                const int64_t at = (int64_t)g * kGroup + (l * 64 + lane) * kPer;
-#pragma unroll
-                for (int e = 0; e < kPer; ++e)
-                    if (!edge || z.has(at + e)) f(x[e], at + e);
-            }
-            end(g);
-        }
-    };
+    const auto over = [&](auto&& f, auto&& end) { over_groups(z, wave, groups, kFlatWaves, f, end); };
     const auto nothing = [](int32_t) {};
 
     // What every span holds: the weights of the tokens whose order exceeds `at_order`, and, of those that have
@@ -901,6 +1067,22 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
                 mine = 0;
                 same = 0;
             });
+        __syncthreads();
+    };
+    // The same from pass 4, a span a group, where its list had room.
+    const bool shared = state == kShared && s.near[row].collected <= min(list_room(s), (uint32_t)kCollected);
+    const auto take_shared = [&] {
+        const uint32_t n = s.near[row].collected;
+        const u64* const list = (const u64*)(s.subs + row * s.groups * kSubs);
+        for (uint32_t i = tid; i < n; i += kFlatThreads) {
+            key[i] = (uint32_t)list[i];
+            place[i] = (uint32_t)(list[i] >> 32);
+        }
+        for (int i = tid; i < kSpans; i += kFlatThreads) {
+            span_sum[i] = i < groups ? ((const u64*)s.sums)[row * s.groups + i] : 0;
+            span_ties[i] = 0;
+        }
+        if (tid == 0) collected = n;
         __syncthreads();
     };
     const auto clear_bins = [&]() {
@@ -951,7 +1133,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
     // sixty: its histogram alone took 70 us.)
     const float steps = (float)(64.0 * w.per);
     const auto near_top = [&](float x) -> uint32_t {
-        return (uint32_t)(kBins - 1) - min((uint32_t)((w.top_f - x) * steps), (uint32_t)(kBins - 1));
+        return (uint32_t)(kBins - 1) - (uint32_t)fminf((w.top_f - x) * steps, (float)(kBins - 1));
     };
     for (int stage = 0; stage < 2; ++stage) {
         if (!(stage == 0 ? r.by_count : r.by_mass)) continue;
@@ -964,7 +1146,11 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
         };
         u64 want = (u64)r.k;
         bool listed = false, limit_in = false;        // a list, and the limit's tokens in it
-        if (top < kKeyInf) {
+        if (shared) {
+            take_shared();
+            want = s.near[row].rest;
+            listed = true;
+        } else if (top < kKeyInf) {
             clear_bins();
             over(
                 [&](float x, int64_t) {
@@ -1030,19 +1216,37 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
             // the cut among the listed tokens
             const int n = min((int)collected, kCollected);
             if (n <= kFlatThreads) {
-                // a token's rank and the worth of those before it, by comparing it with each
-                const uint32_t k = tid < n ? key[tid] : 0, at = tid < n ? place[tid] : 0;
-                u64 before = 0;
-                uint32_t same_before = 0;
-                for (int i = 0; i < n; ++i) {
-                    const uint32_t other = key[i];
-                    const bool same = other == k && place[i] < at;
-                    if (other > k || same) before += worth(other);
-                    same_before += same;
+                // A token's rank by comparing it with each, then the mass before it by a sum over the
+                // tokens in that order.  Those that have the limit's key come last, and the first
+                // limit_ties of them count.
+                const uint32_t k = tid < n ? key[tid] : 0;
+                u64* const order = bin_weight;               // done with
+                u64* const ranked = bin_weight + kFlatThreads;
+                u64* const sums = ranked + kFlatThreads;
+                const u64 own = tid < n ? (u64)k << 32 | (uint32_t)~place[tid] : 0;
+                order[tid] = own;
+                ranked[tid] = 0;
+                __syncthreads();
+                uint32_t rank = 0;
+                if (wave * 64 < n) {
+                    for (int i = 0; i < n; i += 16) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) rank += order[i + e] > own;
+                    }
                 }
-                const bool at_limit = by_weight && limit != 0 && k == limit;
-                if (at_limit) before += min((u64)same_before, limit_ties) * limit_weight;
-                const bool kept = tid < n && before < want && !(at_limit && same_before >= limit_ties);
+                u64 before = rank;
+                bool counts = true;
+                if (by_weight) {
+                    const uint32_t more = block.count(k > limit);
+                    counts = k > limit || rank - more < limit_ties;
+                    if (tid < n) ranked[rank] = k > limit ? weight_of(value_of(k)) : counts ? limit_weight : 0;
+                    __syncthreads();
+                    u64 all;
+                    sums[tid] = block.before(ranked[tid], block.u, &all);
+                    __syncthreads();
+                    if (tid < n) before = sums[rank];
+                }
+                const bool kept = tid < n && before < want && counts;
                 prefix = block.min(kept ? k : ~0u);
                 want = block.count(kept && k == prefix);
                 cut = prefix;
@@ -1084,7 +1288,12 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
             ties = by_weight && cut == limit ? min(m, limit_ties) : m;
         }
     }
-    if (!r.by_count && !r.by_mass) survey([](float x) { return key_of(x); }, 0, true, 0);
+    if (!r.by_count && !r.by_mass) {
+        if (shared)
+            take_shared();
+        else
+            survey([](float x) { return key_of(x); }, 0, true, 0);
+    }
     const u64 cut_weight = cut != 0 ? kept_weight(value_of(cut)) : 0;
     const u64 here = tid < spans ? span_ties[tid] : 0;
     u64 total;
@@ -1114,44 +1323,31 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
         }
         return;
     }
-    const u64 target = share(u, total, false);     // the running sum has to exceed it
+    const u64 all_kept = total, target = share(u, total, false);     // the running sum has to exceed it
     if (sum > 0 && before <= target && before + sum > target) {
         pick[0] = (u64)tid;
         pick[1] = before;
         pick[2] = ties_before;
     }
     __syncthreads();
-    // the span's tokens in order, 64 at a time
-    if (wave == 0) {
-        u64 run = pick[1], seen = pick[2];
-        const int64_t from = (int64_t)pick[0] * per_span * kGroup, to = min(from + (int64_t)per_span * kGroup,
-                                                                          z.vocab + z.shift);
-        for (int64_t at = from; at < to; at += 64) {
-            const bool in = at + lane < to && z.has(at + lane);
-            const float x = in ? z(at + lane) : -INFINITY;
-            const uint32_t k = in ? key_of(x) : 0;
-            const u64 tied = __ballot(in && k == cut);
-            const u64 rank = seen + __popcll(tied & ((1ull << lane) - 1));
-            u64 y = 0;
-            if (in && (k > cut || (k == cut && rank < ties))) {
-                y = kept_weight(x);
-            }
-            u64 upto = y;
-            for (int d = 1; d < 64; d <<= 1) {
-                const u64 up = (u64)__shfl_up((long long)upto, d);
-                if (lane >= d) upto += up;
-            }
-            const u64 passes = __ballot(run + upto > target);
-            if (passes) {
-                if (lane == __builtin_ctzll(passes)) {
-                    a.out_token[row] = (int32_t)(at + lane - z.shift);
-                    if (a.out_prob) a.out_prob[row] = (float)((double)y / (double)total);
-                }
-                break;
-            }
-            run += (u64)__shfl((long long)upto, 63);
-            seen += __popcll(tied);
+    // the span's tokens in order
+    u64 run = pick[1], seen = pick[2];
+    const int64_t from = (int64_t)pick[0] * per_span * kGroup;
+    const int64_t to = min(from + (int64_t)per_span * kGroup, z.vocab + z.shift);
+    for (int64_t at = from + tid; at - tid < to && run <= target; at += kFlatThreads) {
+        const bool in = at < to && z.has(at);
+        const float x = in ? z(at) : -INFINITY;
+        const uint32_t k = in ? key_of(x) : 0;
+        u64 tied;
+        const u64 rank = seen + block.before((u64)(in && k == cut), block.u, &tied);
+        const u64 y = in && (k > cut || (k == cut && rank < ties)) ? kept_weight(x) : 0;
+        const u64 upto = run + block.before(y, block.u, &total);
+        if (upto <= target && upto + y > target) {
+            a.out_token[row] = (int32_t)(at - z.shift);
+            if (a.out_prob) a.out_prob[row] = (float)((double)y / (double)all_kept);
         }
+        run += total;
+        seen += tied;
     }
 }
 
@@ -1160,23 +1356,53 @@ int32_t most_groups(int64_t vocab) { return (int32_t)((vocab + 7 + kGroup - 1) /
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 
 template <int kType>
-hipError_t sample(const SampleArgs& a, const Stats& s, int32_t per_wave, int bits, hipStream_t stream) {
+hipError_t sample(const SampleArgs& a, const Stats& s, int32_t per_wave, int bits, int cus, hipStream_t stream) {
     const int32_t tiles = (s.groups + per_wave * kScanWaves - 1) / (per_wave * kScanWaves);
     asd_sample_scan_kernel<kType><<<(unsigned)(a.rows * tiles), kScanThreads, 0, stream>>>(a, s, per_wave, tiles);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
     asd_sample_pick_kernel<kType><<<(unsigned)a.rows, kPickThreads, 0, stream>>>(a, s);
     if ((err = hipGetLastError()) != hipSuccess) return err;
+    if (s.queued) {
+        const unsigned grid = (unsigned)cus * 4;
+        asd_sample_part_kernel<kType, false><<<grid, kPartThreads, 0, stream>>>(a, s, bits);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
+        asd_sample_part_kernel<kType, true><<<grid, kPartThreads, 0, stream>>>(a, s, bits);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
+    }
     asd_sample_flat_kernel<kType><<<(unsigned)a.rows, kFlatThreads, 0, stream>>>(a, s, bits);
     return hipGetLastError();
 }
 
 }  // namespace
 
+// The workspace's parts, from `base` on (which may be null to add them up).
+static size_t lay_out(int64_t vocab, int64_t rows, char* base, Stats* s) {
+    const size_t n = (size_t)rows, groups = (size_t)most_groups(vocab) * n;
+    size_t at = 0;
+    const auto part = [&](size_t bytes) {
+        char* const p = base + at;
+        at += align256(bytes);
+        return p;
+    };
+    *s = Stats{};
+    s->groups = most_groups(vocab);
+    s->sums = (double*)part(groups * sizeof(double));
+    s->subs = (uint32_t*)part(groups * kSubs * sizeof(uint32_t));
+    s->tops = (uint32_t*)part(groups * sizeof(uint32_t));
+    s->flat = (int32_t*)part(n * sizeof(int32_t));
+    if (shares_out(vocab)) {
+        s->queued = (uint32_t*)part(sizeof(uint32_t));
+        s->queue = (int32_t*)part(n * sizeof(int32_t));
+        s->near = (Near*)part(n * sizeof(Near));
+        s->bins = (u64*)part(n * kNearBins * sizeof(u64));
+    }
+    return at;
+}
+
 size_t sample_workspace_bytes(int64_t vocab, int64_t rows, int) {
-    const size_t groups = (size_t)most_groups(vocab) * (size_t)rows;
-    return align256(groups * sizeof(double)) + align256(groups * kSubs * 4) + align256(groups * 4) +
-           align256((size_t)rows * 4);
+    Stats s;
+    return lay_out(vocab, rows, nullptr, &s);
 }
 
 hipError_t launch_sample(const SampleArgs& a, asd_dtype dtype, void* workspace, int cus, hipStream_t stream) {
@@ -1184,24 +1410,16 @@ hipError_t launch_sample(const SampleArgs& a, asd_dtype dtype, void* workspace, 
     while (((int64_t)1 << (62 - bits)) < a.vocab) --bits;
     if (bits > 50) bits = 50;
     Stats s;
-    s.groups = most_groups(a.vocab);
-    const size_t groups = (size_t)s.groups * (size_t)a.rows;
-    char* p = (char*)workspace;
-    s.sums = (double*)p;
-    p += align256(groups * sizeof(double));
-    s.subs = (uint32_t*)p;
-    p += align256(groups * kSubs * 4);
-    s.tops = (uint32_t*)p;
-    p += align256(groups * 4);
-    s.flat = (int32_t*)p;
+    lay_out(a.vocab, a.rows, (char*)workspace, &s);
+    const int64_t groups = (int64_t)s.groups * a.rows;
     // groups a wavefront takes: as many as leave eight workgroups to a compute unit, eight at most
-    int64_t per_wave = (int64_t)groups / ((int64_t)cus * 8 * kScanWaves);
+    int64_t per_wave = groups / ((int64_t)cus * 8 * kScanWaves);
     per_wave = per_wave < 1 ? 1 : per_wave > 8 ? 8 : per_wave;
     while (a.rows * ((s.groups + per_wave * kScanWaves - 1) / (per_wave * kScanWaves)) >= ((int64_t)1 << 31))
         per_wave *= 2;
-    if (dtype == ASD_F32) return sample<ASD_F32>(a, s, (int32_t)per_wave, bits, stream);
-    if (dtype == ASD_BF16) return sample<ASD_BF16>(a, s, (int32_t)per_wave, bits, stream);
-    return sample<ASD_F16>(a, s, (int32_t)per_wave, bits, stream);
+    if (dtype == ASD_F32) return sample<ASD_F32>(a, s, (int32_t)per_wave, bits, cus, stream);
+    if (dtype == ASD_BF16) return sample<ASD_BF16>(a, s, (int32_t)per_wave, bits, cus, stream);
+    return sample<ASD_F16>(a, s, (int32_t)per_wave, bits, cus, stream);
 }
 
 }  // namespace asd
