@@ -358,26 +358,15 @@ template <int kN> struct Block {
         for (int w = 0; w < kWaves; ++w) all += u[w];
         return all;
     }
-    // Sums with one barrier: of a number that each wavefront has, and of one that each thread has.  The
-    // place alternates with `turn`, which the caller counts up, so that a wavefront that is ahead does not
-    // write what another still reads.
+    // The sum of a number that each wavefront has, with one barrier: the place alternates with `turn`, which the
+    // caller counts up, so that a wavefront that is ahead does not write what another still reads.
     u64 votes_of[2][kWaves];
-    double masses_of[2][kWaves];
     __device__ __forceinline__ u64 votes(u64 of_wave, int turn) {
         if ((threadIdx.x & 63) == 0) votes_of[turn & 1][threadIdx.x >> 6] = of_wave;
         __syncthreads();
         u64 sum = 0;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) sum += votes_of[turn & 1][w];
-        return sum;
-    }
-    __device__ __forceinline__ double mass(double v, int turn) {
-        v = wave_sum(v);
-        if ((threadIdx.x & 63) == 0) masses_of[turn & 1][threadIdx.x >> 6] = v;
-        __syncthreads();
-        double sum = 0.0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) sum += masses_of[turn & 1][w];
         return sum;
     }
     // sum over the threads before this one, and over all
@@ -445,7 +434,8 @@ __device__ __forceinline__ float inside_unit(float u) {
 constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64, kListed = 2048, kHeld = 8;
 constexpr int kMostSubs = kPickThreads * kHeld;          // sub-block maxima held in registers
 constexpr int kFewest = 192;                             // sub-blocks that candidates come from without top-k
-constexpr int kRanked = 2;                               // candidates a thread ranks by comparing each with each
+constexpr int kRanked = kListed / kPickThreads, kRankBins = 1024;
+static_assert(kMostSubs / 2 * (kSub / 4) / 64 <= kRankBins, "the vectors' starts");
 // Tokens that top-k may ask for here: as many sub-block maxima have to reach the threshold, which the
 // candidates then exceed by -ln(1 - k / subs) / (k / subs), 2.0 at 0.8, where the row is in no order.
 __device__ __forceinline__ int32_t most_k(int32_t subs) { return min(subs * 4 / 5, 1200); }
@@ -459,10 +449,11 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     __shared__ double weight[kListed];
     __shared__ union {
         int32_t wanted[kMostSubs / 2];                       // the sub-blocks to read, then
-        double ranked[kRanked * kPickThreads];               // the weights in order
+        u64 order[kListed];                                  // the candidates by their keys' bins, then
+        double ranked[kListed];                              // the weights in order
     } share;
     int32_t* const wanted = share.wanted;
-    __shared__ uint32_t starts[kMostSubs / 2 * (kSub / kPer) / 64];
+    __shared__ uint32_t starts[kRankBins + 1];               // by 64 vectors of those, then by bin
     __shared__ int32_t found;
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_of_block();
     const int64_t row = blockIdx.x;
@@ -688,112 +679,85 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
         return;
     }
 
-    const int each = (n + kPickThreads - 1) / kPickThreads, from = min(n, tid * each), to = min(n, from + each);
-    if (n <= kRanked * kPickThreads) {
-        // Few: a candidate's rank by comparing its key with each, a compare and an addition with carry; the
-        // weights before it by a sum over the weights in that order.
-        uint32_t rank[kRanked];
-        if (r.by_count || r.by_mass) {
-            if (tid < 64 && n + tid < (n + 63 & ~63)) key[n + tid] = 0;
-            for (int i = tid; i < kRanked * kPickThreads; i += kPickThreads) share.ranked[i] = 0.0;
-            __syncthreads();
-#pragma unroll
-            for (int c = 0; c < kRanked; ++c) {
-                rank[c] = 0;
-                const int base = c * kPickThreads + wave * 64;
-                if (base >= n) break;
-                const uint32_t own = key[base + lane];
-                for (int j0 = 0; j0 < n; j0 += 64) {
-                    // of equal keys the earlier ranks first: those before this one count from its own key on
-                    const uint32_t bound = j0 < base ? own - 1 : own;
-                    if (j0 != base) {
-#pragma unroll 16
-                        for (int j = 0; j < 64; ++j) rank[c] += key[j0 + j] > bound;
-                    } else {
-#pragma unroll 16
-                        for (int j = 0; j < 64; ++j) rank[c] += key[j0 + j] > (j < lane ? own - 1 : own);
-                    }
-                }
-                if (base + lane < n && (!r.by_count || rank[c] < (uint32_t)r.k))
-                    share.ranked[rank[c]] = weight[base + lane];
-            }
-            __syncthreads();
-            if (r.by_mass) {
-                double of[kRanked], mine = 0.0, whole;
-#pragma unroll
-                for (int c = 0; c < kRanked; ++c) mine += of[c] = share.ranked[tid * kRanked + c];
-                double before = block.before(mine, block.d, &whole);
-                if (r.by_count) all = whole;
-#pragma unroll
-                for (int c = 0; c < kRanked; ++c) {
-                    share.ranked[tid * kRanked + c] = before;
-                    before += of[c];
-                }
-                __syncthreads();
-            }
-        }
-        const double goal = (double)r.p * all;
+    uint32_t rank[kRanked];
+    if (r.by_count || r.by_mass) {
+        // Their order: bins of one width in the logit, from the greatest down, put them in their places but for
+        // those that share a bin, which are compared with each other.  (Comparing each with each took 8 us of
+        // a row's 14, cuts by bisection over the keys' bits 30 of 65 with 1,400 candidates.)
+        const float high = value_of(top), per_bin = kRankBins / (high - value_of(least));
+        const auto bin_of = [&](uint32_t k) {
+            return (uint32_t)fminf(fmaxf((high - value_of(k)) * per_bin, 0.0f), (float)(kRankBins - 1));
+        };
+        for (int b = tid; b < kRankBins; b += kPickThreads) starts[b] = 0;
+        __syncthreads();
+        uint32_t bin[kRanked];
 #pragma unroll
         for (int c = 0; c < kRanked; ++c) {
             const int i = c * kPickThreads + tid;
             if (i >= n) break;
-            if (weight[i] < floor || (r.by_count && rank[c] >= (uint32_t)r.k) ||
-                (r.by_mass && rank[c] != 0 && !(share.ranked[rank[c]] < goal)))
-                weight[i] = 0.0;
+            bin[c] = bin_of(key[i]);
+            rank[c] = atomicAdd(&starts[bin[c]], 1u);
         }
-    } else {
-        // The greatest key that enough tokens, or tokens of enough weight, reach, bit by bit from the first
-        // in which the candidates differ; the first `ties` of those that have it are kept.
-        const int first_bit = top == least ? -1 : 31 - __builtin_clz(top ^ least);
-        const uint32_t common = first_bit == 31 ? 0u : top & ~((2u << max(first_bit, 0)) - 1u);
-        const uint32_t start = first_bit < 0 ? top : common;
-        const auto above = [&](uint32_t bound) {          // weight of the keys greater than it
-            double x = 0.0;
-            for (int i = tid; i < n; i += kPickThreads)
-                if (key[i] > bound) x += weight[i];
-            return block.mass(x, turn++);
-        };
-        const auto reaching = [&](uint32_t bound) {       // tokens whose keys reach it
-            uint32_t c = 0;
-            for (int i = 0; i < n; i += kPickThreads)
-                c += (uint32_t)__popcll(__ballot(i + tid < n && key[i + tid] >= bound));
-            return (uint32_t)block.votes(c, turn++);
-        };
-        uint32_t cut = 0;
-        int32_t ties = 0x7fffffff;
-        double beyond = 0.0;                // weight of the tokens at the count's cut that it leaves out
-        if (r.by_count) {
-            cut = start;
-            for (int bit = first_bit; bit >= 0; --bit)
-                if (reaching(cut | 1u << bit) >= (uint32_t)r.k) cut |= 1u << bit;
-            const int32_t more = (int32_t)reaching(cut + 1);
-            ties = r.k - more;
-            const double one = w(value_of(cut));
-            beyond = ((int32_t)reaching(cut) - r.k) * one;
-            all = above(cut) + ties * one;
+        __syncthreads();
+        static_assert(kRankBins == 2 * kPickThreads, "two bins a thread");
+        const int32_t one = (int32_t)starts[2 * tid], two = (int32_t)starts[2 * tid + 1];
+        int32_t in_all;
+        const int32_t first = block.before(one + two, (int32_t*)block.u, &in_all);
+        starts[2 * tid] = (uint32_t)first;
+        starts[2 * tid + 1] = (uint32_t)(first + one);
+        if (tid == 0) starts[kRankBins] = (uint32_t)n;
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < kRanked; ++c) {
+            const int i = c * kPickThreads + tid;
+            if (i >= n) break;
+            share.order[starts[bin[c]] + rank[c]] = (u64)key[i] << 32 | (uint32_t)~i;
         }
-        if (r.by_mass && (r.by_count || sum >= (double)r.p * all)) {
-            const double goal = (double)r.p * all;
-            uint32_t t = start;
-            for (int bit = first_bit; bit >= 0; --bit) {
-                const uint32_t trial = t | 1u << bit;
-                const double reach = above(trial - 1) - (trial <= cut ? beyond : 0.0);
-                if (reach >= goal && reach > 0.0) t = trial;
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < kRanked; ++c) {
+            const int i = c * kPickThreads + tid;
+            if (i >= n) break;
+            const u64 own = (u64)key[i] << 32 | (uint32_t)~i;
+            const uint32_t from = starts[bin[c]], to = starts[bin[c] + 1];
+            rank[c] = from;
+            for (uint32_t j = from; j < to; ++j) rank[c] += share.order[j] > own;
+        }
+        if (r.by_mass) {
+            // the weights before each, by a sum in that order
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < kRanked; ++c) {
+                const int i = c * kPickThreads + tid;
+                if (i < n) share.ranked[rank[c]] = !r.by_count || rank[c] < (uint32_t)r.k ? weight[i] : 0.0;
             }
-            const double one = w(value_of(t)), missing = goal - above(t);
-            const int32_t m = max(1, one > 0.0 ? (int32_t)min(ceil(missing / one), 2e9) : 1);
-            ties = t == cut ? min(ties, m) : m;
-            cut = t;
+            __syncthreads();
+            double of[kRanked], mine = 0.0, whole;
+#pragma unroll
+            for (int c = 0; c < kRanked; ++c) mine += of[c] = tid * kRanked + c < n ? share.ranked[tid * kRanked + c] : 0.0;
+            double before = block.before(mine, block.d, &whole);
+            if (r.by_count) all = whole;
+#pragma unroll
+            for (int c = 0; c < kRanked; ++c) {
+                share.ranked[tid * kRanked + c] = before;
+                before += of[c];
+            }
+            __syncthreads();
         }
-        int32_t seen = 0, total_cut;
-        for (int i = from; i < to; ++i) seen += key[i] == cut;
-        seen = block.before(seen, (int32_t*)block.u, &total_cut);
-        for (int i = from; i < to; ++i)
-            if (key[i] < cut || (key[i] == cut && seen++ >= ties) || weight[i] < floor) weight[i] = 0.0;
+    }
+    const double goal = (double)r.p * all;
+#pragma unroll
+    for (int c = 0; c < kRanked; ++c) {
+        const int i = c * kPickThreads + tid;
+        if (i >= n) break;
+        if (weight[i] < floor || (r.by_count && rank[c] >= (uint32_t)r.k) ||
+            (r.by_mass && rank[c] != 0 && !(share.ranked[rank[c]] < goal)))
+            weight[i] = 0.0;
     }
     __syncthreads();
 
     // The draw, in order: a thread takes neighbouring candidates.
+    const int each = (n + kPickThreads - 1) / kPickThreads, from = min(n, tid * each), to = min(n, from + each);
     mine = 0.0;
     for (int i = from; i < to; ++i) mine += weight[i];
     double total;

@@ -180,3 +180,57 @@ def test_empty_and_scalar_arguments():
             ((0.5, torch.float32), (10, torch.int32), (0.9, torch.float32), (0.01, torch.float32))]
     b = asd.asd_sample(z, u, temperature=full[0], top_k=full[1], top_p=full[2], min_p=full[3])
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab,pad", [(65537, 0), (70001, 3), (129280, 0), (262130, 0), (262144, 0)])
+def test_flat_rows_of_wide_vocabularies(dtype, vocab, pad):
+    """Rows that many workgroups read in parts, and the widths beside which one does."""
+    z, u = rows_of(6, vocab, dtype, vocab, sigma=1.5, pad=pad)
+    u[0], u[1] = 0.0, 1.0 - 2.0 ** -24
+    check(z, u, p=[0.5, 0.9, 0.95, 0.99, 0.999999, 0.3])
+    check(z, u, m=[1e-2, 1e-3, 1e-4, 1e-6, 2e-3, 1e-9])
+    check(z, u, t=[0.9, 1.0, 1.3, 2.0, 8.0, 1e3], p=0.9, m=[0.0, 1e-3, 1e-4, 0.0, 0.05, 0.5])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_wide_rows_of_few_values_and_in_order(dtype):
+    vocab = 80000
+    gen = torch.Generator().manual_seed(11)
+    z = torch.zeros(9, vocab)
+    z[1, ::3] = -1.0                                              # two values
+    z[2] = torch.randint(0, 9, (vocab,), generator=gen).float()   # nine: more ties than a list holds
+    z[3] = torch.linspace(-6, 6, vocab)                           # in order
+    z[4] = torch.linspace(6, -6, vocab)
+    z[5] = torch.randn(vocab, generator=gen)
+    z[5, 1000:70000] = -math.inf                                  # sub-blocks of nothing
+    z[6] = torch.randn(vocab, generator=gen)
+    z[6, 777] = math.inf
+    z[7] = torch.randn(vocab, generator=gen) * 1e4                # nearly greedy
+    z[8, :64] = 1.0                                               # one sub-block stands out
+    z = z.to(dtype).to(DEV)
+    u = torch.rand(9, generator=gen)
+    for p in (0.2, 0.7, 0.95, 0.9999):
+        check(z, u, p=p)
+        check(z, u, p=p, m=0.01)
+    for m in (0.5, 0.01, 1e-5):
+        check(z, u, m=m)
+
+
+def test_wide_flat_rows_in_a_graph():
+    z, u = rows_of(40, 100003, torch.bfloat16, 5)
+    uniform = u.to(DEV)
+    p = torch.full((40,), 0.95, device=DEV)
+    want = [asd.asd_sample(z, uniform, top_p=p).tolist()]
+    out = torch.empty(40, dtype=torch.int32, device=DEV)
+    space = torch.empty(asd.asd_sample_workspace_bytes(z.dtype, 100003, 40), dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        asd.asd_sample(z, uniform, top_p=p, out_token=out, workspace=space)
+    uniform.copy_(uniform.flip(0))
+    want.append(asd.asd_sample(z, uniform, top_p=p).tolist())
+    for turn in (1, 0, 1, 0):
+        uniform.copy_((u if turn == 0 else u.flip(0)).to(DEV))
+        space.fill_(0xa5)
+        graph.replay()
+        assert out.tolist() == want[turn]
