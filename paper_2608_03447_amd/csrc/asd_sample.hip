@@ -107,8 +107,8 @@ struct Row {
     }
 };
 
-// Who draws a row's token: pass 2, one workgroup of pass 5, or passes 3 and 4, and pass 5 from what they leave.
-enum { kDone = 0, kAlone = 1, kShared = 2 };
+// Rows that pass 2 leaves: to one workgroup each, or to be read in parts by many.
+enum { kAlone = 0, kShared = 1 };
 
 // A shared row's bins: of one width in the logit, counted up to the last one, which all from `high` on are in.
 constexpr int kNearBins = 1024;
@@ -127,14 +127,17 @@ struct Stats {
     uint32_t* subs;        // [rows][groups * kSubs]
     uint32_t* tops;        // [rows][groups]
     double* sums;          // [rows][groups]
-    int32_t* flat;         // [rows]: kDone, or who has the row next
+    uint32_t* queued;      // [2]: rows that pass 2 leaves, by kAlone and kShared,
+    int32_t* queue[2];     // [rows]: and which
     int32_t groups;        // of the row that has most: its first vector may begin before it
     // where rows are shared out (shares_out(vocab)), else null:
-    uint32_t* queued;      // how many such rows,
-    int32_t* queue;        // [rows] and which
     Near* near;            // [rows]
     u64* bins;             // [rows][kNearBins]: weights by their bin
 };
+
+__device__ __forceinline__ void enqueue(const Stats& s, int to, int64_t row) {
+    s.queue[to][atomicAdd(s.queued + to, 1u)] = (int32_t)row;
+}
 
 // A row as 16-byte vectors: its elements stand `shift` places behind the vector grid's origin.
 template <typename T> struct Grid {
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(kScanThreads) void asd_sample_scan_kernel(SampleArg
     const int lane = threadIdx.x & 63, wave = wave_of_block();
     const int64_t row = blockIdx.x / tiles;
     const int32_t tile = (int32_t)(blockIdx.x - row * tiles);
-    if (s.queued && blockIdx.x == 0 && threadIdx.x == 0) *s.queued = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 2) s.queued[threadIdx.x] = 0;
     const Grid<T> z(a, row);
     const Row r(a, row);
     const bool whole = !r.greedy && !r.by_count;
@@ -467,7 +470,6 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
         a.out_token[row] = at < 0 ? -1 : (int32_t)(at - z.shift);
         if (a.out_prob) a.out_prob[row] = (float)prob;
     };
-    if (tid == 0) s.flat[row] = kDone;
 
     uint32_t top = 0;
     for (int32_t g = tid; g < groups; g += kPickThreads) top = max(top, tops[g]);
@@ -539,7 +541,7 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     // Candidates: every token whose key reaches `least`, which `need` sub-blocks' maxima do.
     const int32_t need = r.by_count ? r.k : max(1, min(kFewest, subs / 2));
     if (subs > kMostSubs || (r.by_count && r.k > most_k(subs))) {
-        if (tid == 0) s.flat[row] = kAlone;
+        if (tid == 0) enqueue(s, kAlone, row);
         return;
     }
     uint32_t held[kHeld];
@@ -649,7 +651,7 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     // shared row begin there; they reach four times as far as the lowest sub-block's maximum, which in rows of
     // any spread leaves 1 in 300 tokens or fewer in a bin.
     const auto leave = [&] {
-        const bool shared = s.queued && !r.by_count && top < kKeyInf;
+        const bool shared = s.near && !r.by_count && top < kKeyInf;
         if (shared) {
             uint32_t low = kKeyNan;
 #pragma unroll
@@ -660,10 +662,9 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
             if (tid == 0) {
                 const float high = value_of(least), range = 4.0f * (high - value_of(low));
                 s.near[row] = Near{high, range > 0.0f ? kNearBins / range : 0.0f, top, 0, 0};
-                s.queue[atomicAdd(s.queued, 1u)] = (int32_t)row;
             }
         }
-        if (tid == 0) s.flat[row] = shared ? kShared : kAlone;
+        if (tid == 0) enqueue(s, shared ? kShared : kAlone, row);
     };
     if (blocks > kMostSubs / 2 || n > kListed) {
         leave();
@@ -863,12 +864,12 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_part_kernel(SampleArg
     __shared__ u64 found[2];
     __shared__ uint32_t listed, start;
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_of_block();
-    const uint32_t rows = *s.queued;
+    const uint32_t rows = s.queued[kShared];
     if (rows == 0) return;
     // parts of 4 groups at least, and two to a workgroup where there are enough
     const uint32_t parts = max(1u, min((2 * gridDim.x + rows - 1) / rows, (uint32_t)s.groups / kPartWaves));
     for (int64_t unit = blockIdx.x; unit < (int64_t)rows * parts; unit += gridDim.x) {
-        const int64_t row = s.queue[unit / parts];
+        const int64_t row = s.queue[kShared][unit / parts];
         const uint32_t part = (uint32_t)(unit % parts);
         const Grid<T> z(a, row);
         const Row r(a, row);
@@ -950,12 +951,150 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_part_kernel(SampleArg
 
 // ------------------------------------------------------------ pass 5
 
+// A shared row's token from what passes 3 and 4 left of it, a workgroup a row and a thread a group: the cut
+// among the listed tokens, in the order of their ranks, then the draw's group and its tokens in order.
+constexpr int kFinishList = 1024, kFinishEach = kFinishList / kPartThreads;
+static_assert(kMostSubs / kSubs <= kPartThreads, "a thread a group");
+
+template <int kType>
+__global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleArgs a, Stats s, int bits) {
+    typedef typename Element<kType>::T T;
+    __shared__ Block<kPartThreads> block;
+    __shared__ u64 order[kFinishList], ranked[kFinishList], kept_in[kPartThreads], pick[2];
+    const int tid = threadIdx.x;
+    const uint32_t rows = s.queued[kShared];
+    for (uint32_t q = blockIdx.x; q < rows; q += gridDim.x) {
+        __syncthreads();
+        const int64_t row = s.queue[kShared][q];
+        const Near near = s.near[row];
+        const float u = inside_unit(a.uniform[row]);
+        const int n = (int)min(near.collected, 1u << 24);
+        // more in the cut's bin than fit, and u = 0, for which even a token of no unit is the first
+        if (n > (int)min(list_room(s), (uint32_t)kFinishList) || u == 0.0f) {
+            if (tid == 0) enqueue(s, kAlone, row);
+            continue;
+        }
+        const Grid<T> z(a, row);
+        const Row r(a, row);
+        const Units weight_of(Weights(value_of(near.top), r.t), bits, near.top);
+        const u64 floor = r.by_floor ? (u64)ceil((double)r.m * (double)(1ull << bits)) : 0;
+        const auto kept_weight = [&](float x) -> u64 {
+            const u64 y = weight_of(x);
+            return y >= floor ? y : 0;
+        };
+        const int32_t groups = z.groups();
+        kept_in[tid] = tid < groups ? ((const u64*)s.sums)[row * s.groups + tid] : 0;
+        uint32_t cut = 0, ties = 0;          // kept: greater keys, and the first `ties` tokens that have it
+        const u64* const list = (const u64*)(s.subs + row * s.groups * kSubs);
+        uint32_t key[kFinishEach], place[kFinishEach];
+        if (r.by_mass) {
+#pragma unroll
+            for (int c = 0; c < kFinishEach; ++c) {
+                const int i = c * kPartThreads + tid;
+                const u64 x = i < n ? list[i] : 0;
+                key[c] = (uint32_t)x;
+                place[c] = (uint32_t)(x >> 32);
+                order[i] = i < n ? (u64)key[c] << 32 | (uint32_t)~place[c] : 0;
+                ranked[i] = 0;
+            }
+            __syncthreads();
+            uint32_t rank[kFinishEach];
+#pragma unroll
+            for (int c = 0; c < kFinishEach; ++c) {
+                rank[c] = 0;
+                if (c * kPartThreads >= n) break;
+                const u64 own = order[c * kPartThreads + tid];
+                for (int i = 0; i < n; i += 16) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) rank[c] += order[i + e] > own;
+                }
+                if (c * kPartThreads + tid < n) ranked[rank[c]] = weight_of(value_of(key[c]));
+            }
+            __syncthreads();
+            u64 of[kFinishEach], sum = 0, whole;
+#pragma unroll
+            for (int c = 0; c < kFinishEach; ++c) sum += of[c] = ranked[tid * kFinishEach + c];
+            u64 before = block.before(sum, block.u, &whole);
+#pragma unroll
+            for (int c = 0; c < kFinishEach; ++c) {
+                ranked[tid * kFinishEach + c] = before;
+                before += of[c];
+            }
+            __syncthreads();
+            uint32_t least = ~0u, same = 0;
+            bool kept[kFinishEach];
+#pragma unroll
+            for (int c = 0; c < kFinishEach; ++c) {
+                kept[c] = c * kPartThreads + tid < n && ranked[rank[c]] < near.rest;
+                if (kept[c]) {
+                    least = min(least, key[c]);
+                    atomicAdd(&kept_in[place[c] / kGroup], kept_weight(value_of(key[c])));
+                }
+            }
+            cut = block.min(least);
+#pragma unroll
+            for (int c = 0; c < kFinishEach; ++c) same += kept[c] && key[c] == cut;
+            ties = block.count(same);
+        }
+        __syncthreads();
+        const u64 mine = kept_in[tid];
+        u64 total, all;
+        const u64 before = block.before(mine, block.u, &all), target = share(u, all, false);
+        if (mine > 0 && before <= target && before + mine > target) {
+            pick[0] = (u64)tid;
+            pick[1] = before;
+        }
+        __syncthreads();
+        const int64_t from = (int64_t)pick[0] * kGroup;
+        u64 run = pick[1];
+        uint32_t seen = 0;                   // tokens that have the cut's key before the group's
+        if (r.by_mass) {
+#pragma unroll
+            for (int c = 0; c < kFinishEach; ++c)
+                seen += c * kPartThreads + tid < n && key[c] == cut && place[c] < (uint32_t)from;
+            seen = block.count(seen);
+        }
+        // a thread four neighbouring tokens
+        constexpr int kEach = kGroup / kPartThreads;
+        uint32_t k[kEach], tied = 0, all_tied;
+        float x[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int64_t at = from + tid * kEach + e;
+            x[e] = z.has(at) ? z(at) : -INFINITY;
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            k[e] = z.has(from + tid * kEach + e) ? key_of(x[e]) : 0;
+            tied += r.by_mass && k[e] == cut;
+        }
+        seen += block.before(tied, (uint32_t*)block.u, &all_tied);
+        u64 y[kEach], sum = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const bool kept = k[e] > cut || (r.by_mass && k[e] == cut && seen++ < ties);
+            sum += y[e] = kept ? kept_weight(x[e]) : 0;
+        }
+        run += block.before(sum, block.u, &total);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            if (run <= target && run + y[e] > target) {
+                a.out_token[row] = (int32_t)(from + tid * kEach + e - z.shift);
+                if (a.out_prob) a.out_prob[row] = (float)((double)y[e] / (double)all);
+            }
+            run += y[e];
+        }
+    }
+}
+
+// ------------------------------------------------------------ pass 6
+
 constexpr int kFlatThreads = 1024, kFlatWaves = kFlatThreads / 64, kBins = 4096, kCollected = 8192, kSpans = 1024;
 
 // A workgroup a row.  Weights are whole numbers of 2^-bits of the greatest, so that sums over any order are
 // the same; spans of `span` tokens (1,024 up to 2^20 tokens a row) hold what is kept of them.
 template <int kType>
-__global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArgs a, Stats s, int bits) {
+__device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, int bits, int64_t row) {
     typedef typename Element<kType>::T T;
     __shared__ Block<kFlatThreads> block;
     __shared__ u64 bin_weight[kBins];
@@ -966,9 +1105,6 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
     __shared__ uint32_t collected;
     __shared__ u64 pick[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_of_block();
-    const int64_t row = blockIdx.x;
-    const int32_t state = s.flat[row];
-    if (state == kDone) return;
     const Grid<T> z(a, row);
     const Row r(a, row);
     const int32_t groups = z.groups(), per_span = (groups + kSpans - 1) / kSpans;
@@ -1033,22 +1169,6 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
             });
         __syncthreads();
     };
-    // The same from pass 4, a span a group, where its list had room.
-    const bool shared = state == kShared && s.near[row].collected <= min(list_room(s), (uint32_t)kCollected);
-    const auto take_shared = [&] {
-        const uint32_t n = s.near[row].collected;
-        const u64* const list = (const u64*)(s.subs + row * s.groups * kSubs);
-        for (uint32_t i = tid; i < n; i += kFlatThreads) {
-            key[i] = (uint32_t)list[i];
-            place[i] = (uint32_t)(list[i] >> 32);
-        }
-        for (int i = tid; i < kSpans; i += kFlatThreads) {
-            span_sum[i] = i < groups ? ((const u64*)s.sums)[row * s.groups + i] : 0;
-            span_ties[i] = 0;
-        }
-        if (tid == 0) collected = n;
-        __syncthreads();
-    };
     const auto clear_bins = [&]() {
         for (int b = tid; b < kBins; b += kFlatThreads) {
             bin_weight[b] = 0;
@@ -1110,11 +1230,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
         };
         u64 want = (u64)r.k;
         bool listed = false, limit_in = false;        // a list, and the limit's tokens in it
-        if (shared) {
-            take_shared();
-            want = s.near[row].rest;
-            listed = true;
-        } else if (top < kKeyInf) {
+        if (top < kKeyInf) {
             clear_bins();
             over(
                 [&](float x, int64_t) {
@@ -1252,12 +1368,7 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
             ties = by_weight && cut == limit ? min(m, limit_ties) : m;
         }
     }
-    if (!r.by_count && !r.by_mass) {
-        if (shared)
-            take_shared();
-        else
-            survey([](float x) { return key_of(x); }, 0, true, 0);
-    }
+    if (!r.by_count && !r.by_mass) survey([](float x) { return key_of(x); }, 0, true, 0);
     const u64 cut_weight = cut != 0 ? kept_weight(value_of(cut)) : 0;
     const u64 here = tid < spans ? span_ties[tid] : 0;
     u64 total;
@@ -1315,6 +1426,15 @@ __global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArg
     }
 }
 
+template <int kType>
+__global__ __launch_bounds__(kFlatThreads) void asd_sample_flat_kernel(SampleArgs a, Stats s, int bits) {
+    const uint32_t rows = s.queued[kAlone];
+    for (uint32_t q = blockIdx.x; q < rows; q += gridDim.x) {
+        flat_row<kType>(a, s, bits, s.queue[kAlone][q]);
+        __syncthreads();
+    }
+}
+
 int32_t most_groups(int64_t vocab) { return (int32_t)((vocab + 7 + kGroup - 1) / kGroup); }
 
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
@@ -1327,14 +1447,18 @@ hipError_t sample(const SampleArgs& a, const Stats& s, int32_t per_wave, int bit
     if (err != hipSuccess) return err;
     asd_sample_pick_kernel<kType><<<(unsigned)a.rows, kPickThreads, 0, stream>>>(a, s);
     if ((err = hipGetLastError()) != hipSuccess) return err;
-    if (s.queued) {
+    if (s.near) {
         const unsigned grid = (unsigned)cus * 4;
         asd_sample_part_kernel<kType, false><<<grid, kPartThreads, 0, stream>>>(a, s, bits);
         if ((err = hipGetLastError()) != hipSuccess) return err;
         asd_sample_part_kernel<kType, true><<<grid, kPartThreads, 0, stream>>>(a, s, bits);
         if ((err = hipGetLastError()) != hipSuccess) return err;
+        asd_sample_finish_kernel<kType>
+            <<<(unsigned)(a.rows < grid ? a.rows : grid), kPartThreads, 0, stream>>>(a, s, bits);
+        if ((err = hipGetLastError()) != hipSuccess) return err;
     }
-    asd_sample_flat_kernel<kType><<<(unsigned)a.rows, kFlatThreads, 0, stream>>>(a, s, bits);
+    asd_sample_flat_kernel<kType>
+        <<<(unsigned)(a.rows < cus ? a.rows : cus), kFlatThreads, 0, stream>>>(a, s, bits);
     return hipGetLastError();
 }
 
@@ -1354,10 +1478,10 @@ static size_t lay_out(int64_t vocab, int64_t rows, char* base, Stats* s) {
     s->sums = (double*)part(groups * sizeof(double));
     s->subs = (uint32_t*)part(groups * kSubs * sizeof(uint32_t));
     s->tops = (uint32_t*)part(groups * sizeof(uint32_t));
-    s->flat = (int32_t*)part(n * sizeof(int32_t));
+    s->queued = (uint32_t*)part(2 * sizeof(uint32_t));
+    s->queue[kAlone] = (int32_t*)part(n * sizeof(int32_t));
     if (shares_out(vocab)) {
-        s->queued = (uint32_t*)part(sizeof(uint32_t));
-        s->queue = (int32_t*)part(n * sizeof(int32_t));
+        s->queue[kShared] = (int32_t*)part(n * sizeof(int32_t));
         s->near = (Near*)part(n * sizeof(Near));
         s->bins = (u64*)part(n * kNearBins * sizeof(u64));
     }
