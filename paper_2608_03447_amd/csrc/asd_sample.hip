@@ -170,14 +170,14 @@ template <typename T>
 __device__ __forceinline__ u32x4 load_vector(const Grid<T>& z, int64_t at) {
     return at < z.vocab + z.shift ? *(const u32x4*)(z.origin + at) : u32x4{0, 0, 0, 0};
 }
-// The vector with -inf in the places outside the row.
+// The vector with -inf, or NaN, in the places outside the row.
 template <typename T>
-__device__ __forceinline__ u32x4 in_row(const Grid<T>& z, int64_t at, u32x4 raw) {
+__device__ __forceinline__ u32x4 in_row(const Grid<T>& z, int64_t at, u32x4 raw, float fill = -INFINITY) {
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) raw[e] = z.has(at + e) ? raw[e] : 0xff800000u;
+        for (int e = 0; e < 4; ++e) raw[e] = z.has(at + e) ? raw[e] : __float_as_uint(fill);
     } else {
-        const uint32_t none = __builtin_bit_cast(unsigned short, (T)-INFINITY);
+        const uint32_t none = __builtin_bit_cast(unsigned short, (T)fill);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             if (!z.has(at + e)) raw[e / 2] = e % 2 ? (raw[e / 2] & 0xffffu) | none << 16 : (raw[e / 2] & 0xffff0000u) | none;
@@ -595,32 +595,33 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     constexpr int kLanes = kSub / kPer, kAhead = 8, kWaves = kPickWaves;
     const int32_t sweeps = (blocks * kLanes + 63) / 64;
     if (blocks <= kMostSubs / 2) {
+        // No NaN is left here, so that the logits' own order is the keys'; one fills places that do not count.
+        const float from = value_of(least);
         const auto sweep = [&](auto&& f) {
             for (int32_t b = wave; b < sweeps; b += kAhead * kWaves) {
                 u32x4 raw[kAhead];
-                int64_t at[kAhead];
+                uint32_t at[kAhead];
 #pragma unroll
                 for (int c = 0; c < kAhead; ++c) {
                     const int32_t v = (b + c * kWaves) * 64 + lane;
-                    at[c] = v < blocks * kLanes ? (int64_t)wanted[v / kLanes] * kSub + v % kLanes * kPer : -1;
-                    raw[c] = at[c] >= 0 ? load_vector(z, at[c]) : u32x4{0, 0, 0, 0};
+                    at[c] = v < blocks * kLanes ? (uint32_t)(wanted[v / kLanes] * kSub + v % kLanes * kPer) : ~0u;
+                    raw[c] = load_vector(z, at[c]);
                 }
 #pragma unroll
                 for (int c = 0; c < kAhead; ++c) {
                     if (b + c * kWaves >= sweeps) break;
+                    if (at[c] < (uint32_t)z.shift || (int64_t)at[c] + kPer > z.vocab + z.shift)
+                        raw[c] = in_row(z, at[c], raw[c], NAN);
                     float x[kPer];
                     unpack<T>(raw[c], x);
-                    uint32_t k[kPer];
-#pragma unroll
-                    for (int e = 0; e < kPer; ++e) k[e] = at[c] >= 0 && z.has(at[c] + e) ? key_of(x[e]) : 0;
-                    f(b + c * kWaves, at[c], k);
+                    f(b + c * kWaves, at[c], x);
                 }
             }
         };
-        sweep([&](int32_t b, int64_t, const uint32_t* k) {
+        sweep([&](int32_t b, uint32_t, const float* x) {
             uint32_t c = 0;
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) c += (uint32_t)__popcll(__ballot(k[e] >= least));
+            for (int e = 0; e < kPer; ++e) c += (uint32_t)__popcll(__ballot(x[e] >= from));
             if (lane == 0) starts[b] = c;
         });
         __syncthreads();
@@ -633,16 +634,18 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
         }
         __syncthreads();
         if (n <= kListed)
-            sweep([&](int32_t b, int64_t at, const uint32_t* k) {
+            sweep([&](int32_t b, uint32_t at, const float* x) {
                 uint32_t to = starts[b];
-                const u64 below = (1ull << lane) - 1;
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) to += (uint32_t)__popcll(__ballot(k[e] >= least) & below);
+                for (int e = 0; e < kPer; ++e) {
+                    const u64 in = __ballot(x[e] >= from);
+                    to = __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, to));
+                }
 #pragma unroll
                 for (int e = 0; e < kPer; ++e)
-                    if (k[e] >= least) {
-                        key[to] = k[e];
-                        place[to] = (uint32_t)(at + e);
+                    if (x[e] >= from) {
+                        key[to] = key_of(x[e]);
+                        place[to] = at + e;
                         ++to;
                     }
             });
@@ -682,12 +685,13 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
 
     uint32_t rank[kRanked];
     if (r.by_count || r.by_mass) {
-        // Their order: bins of one width in the logit, from the greatest down, put them in their places but for
-        // those that share a bin, which are compared with each other.  (Comparing each with each took 8 us of
+        // Their order: bins of the logit, from the greatest down and narrower where there are more, put them in
+        // their places but for those that share a bin, which are compared with each other.  (Comparing each with each took 8 us of
         // a row's 14, cuts by bisection over the keys' bits 30 of 65 with 1,400 candidates.)
-        const float high = value_of(top), per_bin = kRankBins / (high - value_of(least));
+        const float low = value_of(least), per = 1.0f / (value_of(top) - low);
         const auto bin_of = [&](uint32_t k) {
-            return (uint32_t)fminf(fmaxf((high - value_of(k)) * per_bin, 0.0f), (float)(kRankBins - 1));
+            const float part = fminf(fmaxf((value_of(k) - low) * per, 0.0f), 1.0f);
+            return (uint32_t)(kRankBins - 1) - (uint32_t)(sqrtf(part) * (float)(kRankBins - 1));
         };
         for (int b = tid; b < kRankBins; b += kPickThreads) starts[b] = 0;
         __syncthreads();
