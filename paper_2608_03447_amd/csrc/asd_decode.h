@@ -73,7 +73,6 @@ struct AttentionArgs {
     uint32_t page_magic;
     int32_t page_shift;
     int32_t team;          // workgroups that share a stretch
-    int32_t resident;      // workgroups that the card holds at once
 };
 size_t attention_workspace_bytes(int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                  int32_t num_requests, int64_t total_rows, int cus);

@@ -130,7 +130,7 @@ struct Stats {
     uint32_t* queued;      // [2]: rows that pass 2 leaves, by kAlone and kShared,
     int32_t* queue[2];     // [rows]: and which
     int32_t groups;        // of the row that has most: its first vector may begin before it
-    // where rows are shared out (shares_out(vocab)), else null:
+    // where rows are shared out (shares_out), else null:
     Near* near;            // [rows]
     u64* bins;             // [rows][kNearBins]: weights by their bin
 };
@@ -220,6 +220,40 @@ __device__ __forceinline__ double wave_sum(double x) {
     a = __builtin_amdgcn_permlane32_swap(u.x, u.x, false, false);
     b = __builtin_amdgcn_permlane32_swap(u.y, u.y, false, false);
     return __builtin_bit_cast(double, u32x2{a.x, b.x}) + __builtin_bit_cast(double, u32x2{a.y, b.y});
+}
+
+// Calls f(value, grid place) for every token of the row's groups g, g + step, ... below `stop`, by one
+// wavefront; a group's end is told by end(group).
+template <typename T, typename F, typename E>
+__device__ __forceinline__ void over_groups(const Grid<T>& z, int32_t g, int32_t stop, int32_t step, F&& f, E&& end) {
+    constexpr int kPer = 16 / sizeof(T), kLoads = kGroup / (64 * kPer);
+    const int lane = threadIdx.x & 63;
+    const int32_t groups = z.groups();
+    if (g >= stop) return;
+    u32x4 next[kLoads];
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) next[l] = load_vector(z, (int64_t)g * kGroup + (l * 64 + lane) * kPer);
+    for (; g < stop; g += step) {
+        u32x4 raw[kLoads];
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) raw[l] = next[l];
+        if (g + step < stop) {
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l)
+                next[l] = load_vector(z, (int64_t)(g + step) * kGroup + (l * 64 + lane) * kPer);
+        }
+        const bool edge = g == 0 || g + 1 >= groups;
+#pragma unroll
+        for (int l = 0; l < kLoads; ++l) {
+            float x[kPer];
+            unpack<T>(raw[l], x);
+            const int64_t at = (int64_t)g * kGroup + (l * 64 + lane) * kPer;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (!edge || z.has(at + e)) f(x[e], at + e);
+        }
+        end(g);
+    }
 }
 
 // ------------------------------------------------------------ pass 1
@@ -439,9 +473,11 @@ constexpr int kMostSubs = kPickThreads * kHeld;          // sub-block maxima hel
 constexpr int kFewest = 192;                             // sub-blocks that candidates come from without top-k
 constexpr int kRanked = kListed / kPickThreads, kRankBins = 1024;
 static_assert(kMostSubs / 2 * (kSub / 4) / 64 <= kRankBins, "the vectors' starts");
-// Tokens that top-k may ask for here: as many sub-block maxima have to reach the threshold, which the
-// candidates then exceed by -ln(1 - k / subs) / (k / subs), 2.0 at 0.8, where the row is in no order.
-__device__ __forceinline__ int32_t most_k(int32_t subs) { return min(subs * 4 / 5, 1200); }
+// Top-k takes its candidates from a threshold that k sub-blocks' maxima reach, for as many as this: in a row in no
+// order -ln(1 - k / subs) / (k / subs) times as many do, 1.53 at 0.6.  Beyond, up to kMostK, from a histogram
+// of the row.
+__device__ __forceinline__ int32_t most_k(int32_t subs) { return min(subs * 3 / 5, 1200); }
+constexpr int32_t kMostK = kListed - 128;
 
 template <int kType>
 __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArgs a, Stats s) {
@@ -538,9 +574,10 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
         all = block.sum(mine);
     }
 
-    // Candidates: every token whose key reaches `least`, which `need` sub-blocks' maxima do.
+    // Candidates: every token whose key reaches `least`; all of a short row.
     const int32_t need = r.by_count ? r.k : max(1, min(kFewest, subs / 2));
-    if (subs > kMostSubs || (r.by_count && r.k > most_k(subs))) {
+    const bool all_listed = z.vocab <= kListed, by_bins = !all_listed && r.by_count && r.k > most_k(subs);
+    if (subs > kMostSubs || (by_bins && (r.k > kMostK || top >= kKeyInf))) {
         if (tid == 0) enqueue(s, kAlone, row);
         return;
     }
@@ -548,23 +585,55 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) held[i] = i * kPickThreads + tid < subs ? sub[i * kPickThreads + tid] : 0;
     int turn = 0;               // of the sums with one barrier
-    uint32_t least = 0;         // by its upper 16 bits, two at a time
-    for (int bit = 30; bit >= 16; bit -= 2) {
-        if ((least | 1u << bit) > top) continue;
-        u64 n = 0;              // how many reach each of the three trials
+    // the least of the sub-blocks' maxima, but of those that hold nothing
+    const auto lowest = [&] {
+        uint32_t low = kKeyNan;
 #pragma unroll
-        for (int i = 0; i < kHeld; ++i) {
-            if (i * kPickThreads >= subs) break;
+        for (int i = 0; i < kHeld; ++i)
+            if (held[i] > kKeyNegInf) low = min(low, held[i]);
+        return block.min(low);
+    };
+    uint32_t least = 0;
+    if (by_bins) {
+        // bins of one width in the logit, from the greatest down to as far below the least of the maxima
+        const float high = value_of(top), per = 0.5f * kRankBins / (high - value_of(lowest()));
+        for (int b = tid; b < kRankBins; b += kPickThreads) starts[b] = 0;
+        __syncthreads();
+        over_groups(
+            z, wave, groups, kPickWaves,
+            [&](float x, int64_t) {
+                atomicAdd(&starts[(uint32_t)fminf(fmaxf((high - x) * per, 0.0f), (float)(kRankBins - 1))], 1u);
+            },
+            [](int32_t) {});
+        __syncthreads();
+        const int32_t one = (int32_t)starts[2 * tid], two = (int32_t)starts[2 * tid + 1];
+        int32_t in_all;
+        const int32_t before = block.before(one + two, (int32_t*)block.u, &in_all);
+        if (before < need && before + one + two >= need) found = 2 * tid + (before + one < need);
+        __syncthreads();
+        // All of that bin and those above it.  A hundredth of a bin further, which is more than the roundings of
+        // the bins' numbers; the difference's own rounding passes no logit.
+        const float edge = high - ((float)found + 1.01f) / per;
+        least = found < kRankBins - 1 && edge > -INFINITY ? key_of(edge) : 0;
+    } else if (!all_listed) {
+        // by its upper 16 bits, two at a time
+        for (int bit = 30; bit >= 16; bit -= 2) {
+            if ((least | 1u << bit) > top) continue;
+            u64 n = 0;              // how many reach each of the three trials
 #pragma unroll
-            for (uint32_t c = 1; c < 4; ++c)
-                n += (u64)__popcll(__ballot(held[i] >= (least | c << bit))) << (20 * (c - 1));
-        }
-        n = block.votes(n, turn++);
-        for (uint32_t c = 3; c > 0; --c)
-            if ((uint32_t)(n >> (20 * (c - 1)) & 0xfffff) >= (uint32_t)need) {
-                least |= c << bit;
-                break;
+            for (int i = 0; i < kHeld; ++i) {
+                if (i * kPickThreads >= subs) break;
+#pragma unroll
+                for (uint32_t c = 1; c < 4; ++c)
+                    n += (u64)__popcll(__ballot(held[i] >= (least | c << bit))) << (20 * (c - 1));
             }
+            n = block.votes(n, turn++);
+            for (uint32_t c = 3; c > 0; --c)
+                if ((uint32_t)(n >> (20 * (c - 1)) & 0xfffff) >= (uint32_t)need) {
+                    least |= c << bit;
+                    break;
+                }
+        }
     }
     least = max(least, kKeyNegInf);
     // the sub-blocks that reach it, in order: the counts of each held[i] of each wavefront, summed up
@@ -656,11 +725,7 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
     const auto leave = [&] {
         const bool shared = s.near && !r.by_count && top < kKeyInf;
         if (shared) {
-            uint32_t low = kKeyNan;
-#pragma unroll
-            for (int i = 0; i < kHeld; ++i)
-                if (held[i] > kKeyNegInf) low = min(low, held[i]);
-            low = block.min(low);
+            const uint32_t low = lowest();
             for (int b = tid; b < kNearBins; b += kPickThreads) s.bins[row * kNearBins + b] = 0;
             if (tid == 0) {
                 const float high = value_of(least), range = 4.0f * (high - value_of(low));
@@ -688,7 +753,14 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
         // Their order: bins of the logit, from the greatest down and narrower where there are more, put them in
         // their places but for those that share a bin, which are compared with each other.  (Comparing each with each took 8 us of
         // a row's 14, cuts by bisection over the keys' bits 30 of 65 with 1,400 candidates.)
-        const float low = value_of(least), per = 1.0f / (value_of(top) - low);
+        uint32_t last = least;
+        if (least == kKeyNegInf) {          // all of the row: from the least logit that has a weight
+            last = kKeyNan;
+            for (int i = tid; i < n; i += kPickThreads)
+                if (key[i] > kKeyNegInf) last = min(last, key[i]);
+            last = block.min(last);
+        }
+        const float low = value_of(last), per = 1.0f / (value_of(top) - low);
         const auto bin_of = [&](uint32_t k) {
             const float part = fminf(fmaxf((value_of(k) - low) * per, 0.0f), 1.0f);
             return (uint32_t)(kRankBins - 1) - (uint32_t)(sqrtf(part) * (float)(kRankBins - 1));
@@ -726,7 +798,12 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
             const u64 own = (u64)key[i] << 32 | (uint32_t)~i;
             const uint32_t from = starts[bin[c]], to = starts[bin[c] + 1];
             rank[c] = from;
-            for (uint32_t j = from; j < to; ++j) rank[c] += share.order[j] > own;
+            uint32_t j = from;
+            for (; j + 4 <= to; j += 4) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) rank[c] += share.order[j + e] > own;
+            }
+            for (; j < to; ++j) rank[c] += share.order[j] > own;
         }
         if (r.by_mass) {
             // the weights before each, by a sum in that order
@@ -812,40 +889,6 @@ struct Units {
     }
 };
 
-// Calls f(value, grid place) for every token of the row's groups g, g + step, ... below `stop`, by one
-// wavefront; a group's end is told by end(group).
-template <typename T, typename F, typename E>
-__device__ __forceinline__ void over_groups(const Grid<T>& z, int32_t g, int32_t stop, int32_t step, F&& f, E&& end) {
-    constexpr int kPer = 16 / sizeof(T), kLoads = kGroup / (64 * kPer);
-    const int lane = threadIdx.x & 63;
-    const int32_t groups = z.groups();
-    if (g >= stop) return;
-    u32x4 next[kLoads];
-#pragma unroll
-    for (int l = 0; l < kLoads; ++l) next[l] = load_vector(z, (int64_t)g * kGroup + (l * 64 + lane) * kPer);
-    for (; g < stop; g += step) {
-        u32x4 raw[kLoads];
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) raw[l] = next[l];
-        if (g + step < stop) {
-#pragma unroll
-            for (int l = 0; l < kLoads; ++l)
-                next[l] = load_vector(z, (int64_t)(g + step) * kGroup + (l * 64 + lane) * kPer);
-        }
-        const bool edge = g == 0 || g + 1 >= groups;
-#pragma unroll
-        for (int l = 0; l < kLoads; ++l) {
-            float x[kPer];
-            unpack<T>(raw[l], x);
-            const int64_t at = (int64_t)g * kGroup + (l * 64 + lane) * kPer;
-#pragma unroll
-            for (int e = 0; e < kPer; ++e)
-                if (!edge || z.has(at + e)) f(x[e], at + e);
-        }
-        end(g);
-    }
-}
-
 // ------------------------------------------------------------ passes 3 and 4
 
 // Rows that keep more tokens than pass 2 holds, by mass alone: every row in parts, all workgroups of the launch
@@ -853,9 +896,12 @@ __device__ __forceinline__ void over_groups(const Grid<T>& z, int32_t g, int32_t
 // is reached, sums each group's weights above it and lists the bin's own tokens.
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPartList = 1024;
 
-// Vocabularies whose rows are shared out: sub-blocks that pass 2 can hold, and rows long enough for two more
-// launches.  One workgroup took 220 us for a row of 129,280.
-bool shares_out(int64_t vocab) { return vocab > 65536 && vocab + 7 <= (int64_t)kMostSubs * kSub; }
+// Whether rows are shared out: where pass 2 can hold their sub-blocks, and they are long, or many, enough to
+// pay for three more launches, 6 us where no row is flat.  One flat row of 32,000 takes 83 us alone, one of
+// 65,000 111 us, one of 151,936 55 us shared out; 300 of 32,000 take 120 us alone.
+bool shares_out(int64_t vocab, int64_t rows) {
+    return vocab > (rows < 8 ? 65536 : 8192) && vocab + 7 <= (int64_t)kMostSubs * kSub;
+}
 
 // Shared tokens of a row that its list has room for, in the place of its sub-blocks' maxima.
 __device__ __forceinline__ uint32_t list_room(const Stats& s) { return (uint32_t)s.groups * (kSubs / 2); }
@@ -1484,7 +1530,7 @@ static size_t lay_out(int64_t vocab, int64_t rows, char* base, Stats* s) {
     s->tops = (uint32_t*)part(groups * sizeof(uint32_t));
     s->queued = (uint32_t*)part(2 * sizeof(uint32_t));
     s->queue[kAlone] = (int32_t*)part(n * sizeof(int32_t));
-    if (shares_out(vocab)) {
+    if (shares_out(vocab, rows)) {
         s->queue[kShared] = (int32_t*)part(n * sizeof(int32_t));
         s->near = (Near*)part(n * sizeof(Near));
         s->bins = (u64*)part(n * kNearBins * sizeof(u64));

@@ -234,3 +234,19 @@ def test_wide_flat_rows_in_a_graph():
         space.fill_(0xa5)
         graph.replay()
         assert out.tolist() == want[turn]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("vocab", [300, 2048, 2049, 3001, 20000, 65000, 100000])
+def test_counts_next_to_the_width(dtype, vocab):
+    """Top-k of few and of most tokens, where neighbouring logits tie or one stands far out."""
+    z, u = rows_of(7, vocab, dtype, vocab + 1)
+    z[1] = z[1].float().round().to(dtype)
+    z[2] = 0.5
+    z[3, 5] = 3e4
+    z[4, vocab // 2:] = -math.inf
+    z[5] += 1000
+    k = [vocab - 1, 1000, 1500, 600, 1900, 1921, vocab // 3]
+    for p in (1.0, 0.9, 0.3):
+        check(z, u, k=k, p=p)
+        check(z, u, k=k[::-1], p=p, m=1e-3, t=1.5)
