@@ -531,7 +531,8 @@ asd_status asd_rope_append(const void *q, const void *k, const void *v, asd_dtyp
  *
  * Scores, maxima, sums and outputs are held in binary32, the weights enter the
  * second product rounded to dtype (as the matrix cores take them) and the
- * output is rounded once.
+ * output is rounded once.  The same call gives the same bits; where a sequence is
+ * cut for the chip's workgroups depends on the batch, and with it a row's last bits.
  *
  * q               row r's heads, dense, at q + r * q_stride (elements, a multiple
  *                 of 8); dtype ASD_BF16 or ASD_F16; 16-byte aligned.
@@ -576,8 +577,10 @@ size_t asd_block_attention_workspace_bytes(int32_t num_q_heads, int32_t num_kv_h
  * and the token drawn is the first, by index, at which the running sum of the
  * kept weights exceeds u times their sum.  T <= 0 or NaN: the row's argmax
  * (lowest index among equals), whatever k, p, min_p and u are.  Weights are
- * held to 2^-44 of the greatest or better and summed without further rounding,
- * so the same row gives the same token in any batch.
+ * held to 2^-44 of the greatest or better and summed in binary64 or as integers, in an order
+ * that depends on the row alone and on its address modulo 16: a token is the one
+ * above unless u, or a cut, lies within 2^-40 of an edge, and a call's other rows
+ * have no part in it.
  *
  * -0 equals +0; a logit of -inf has no weight; where the greatest is +inf the
  * tokens at +inf share the weight.  A row that holds a NaN, or nothing but -inf,

@@ -1,21 +1,29 @@
 // gfx950 kernels that draw a token from every logit row.
 //
-// Pass 1 (asd_sample_scan_kernel) reads every row once from HBM, a wavefront a group
-// of 1,024 logits at a time, and leaves the greatest logit of every 64 (a
-// sub-block) and, for rows whose whole mass counts, the group's sum of
-// exp((z - its greatest) / T) in binary64.
+// Nothing is sorted as a whole: the running sum of the draw is taken in index order, and what the filters cut is
+// found among the few tokens next to the cut.
 //
-// Pass 2 (asd_sample_pick_kernel), a workgroup a row, works on those: without filters the draw
-// falls into one group, which is read again; with them, a threshold that as many sub-block
-// maxima reach as tokens are wanted bounds the candidates from below, only the sub-blocks
-// whose maximum reaches it are read again, and the filters' cuts are found among the
-// candidates by bisection over the logits' keys.  Rows that keep too many tokens for that (a nucleus of
-// tens of thousands) are left to
+// Pass 1 (scan) reads every row once from HBM, a wavefront a group of 1,024 logits at a
+// time, and leaves the greatest logit of every 64 (a sub-block) and, for rows whose whole mass counts, the
+// group's sum of exp((z - its greatest) / T) in binary64.
 //
-// Pass 3 (asd_sample_flat_kernel): a histogram of the row's weights over its keys' leading bits gives the
-// bin that holds the cut, a second reading collects that bin and sums what lies above it.
+// Pass 2 (pick), a workgroup a row, works on those: without filters the draw falls into one group, which is
+// read again; with them, a threshold that as many sub-block maxima reach as tokens are wanted bounds the
+// candidates from below, only the sub-blocks whose maximum reaches it are read again, and the filters' cuts
+// are found among the candidates, up to 2,048, by their order.
 //
-// The running sum is taken in index order, so nothing is sorted.
+// Rows that keep more tokens than that (a nucleus of tens of thousands) are read again in parts by all workgroups: pass
+// 3 sums their weights by bins of the logit, pass 4 lists the tokens of the bin that holds the cut and sums, group by
+// group, what lies above it, and pass 5 (finish) finds the cut among the listed and draws.  Pass 6 (flat), one
+// workgroup a row, takes what is left: calls too small for passes 3 to 5, top-k beyond 1,920, bins of more
+// ties than a list holds.
+//
+// Bounds and measurements: pass 1 is memory's and the binary64 exponentials'; 2,112 rows of 151,936 float32
+// (1.28 GB) take 267 us, 4.8 TB/s.  Pass 2 is latency and, with 1,400 candidates, arithmetic: 12 us for
+// one row of 32,000 with top-k 50, 36 with top-k 1,000 of 129,280, 110 for the 2,112.  Passes 3 and 4 are
+// the exponentials': 74 and 83 us for some 480 flat rows of the 2,112, 9 and 12 for 15 rows of 129,280 in bfloat16;
+// pass 5 26 and 11.  In all 535 us, 85 us for 67 rows of 129,280, 17.7 for one of 32,000 (a bisection over
+// each row by one workgroup took 7,165, 584 and 202).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -1141,8 +1149,9 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleA
 
 constexpr int kFlatThreads = 1024, kFlatWaves = kFlatThreads / 64, kBins = 4096, kCollected = 8192, kSpans = 1024;
 
-// A workgroup a row.  Weights are whole numbers of 2^-bits of the greatest, so that sums over any order are
-// the same; spans of `span` tokens (1,024 up to 2^20 tokens a row) hold what is kept of them.
+// A whole row by one workgroup: histograms of it give the bin that holds the cut, a second reading lists that bin
+// and sums what lies above it.  Each reading of 129,280 logits takes 50 us, the exponentials' time on one
+// compute unit.  Spans (1,024 tokens each up to 2^20 tokens a row) hold what is kept of them.
 template <int kType>
 __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, int bits, int64_t row) {
     typedef typename Element<kType>::T T;
