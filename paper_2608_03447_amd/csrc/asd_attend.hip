@@ -24,7 +24,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 // Bounds and measurements (128-element heads in bfloat16, 32 query heads to 8 key heads unless said):
 //  - single tokens and blocks: the cache's bytes.  64 single tokens over up to 8,192: 218 us, 4.9 TB/s where a
 //    plain read reaches 6.9; some 25 us of it are the batch's sharing out, each item's first loads and the
-//    join.  9 rows over 65,000: 81 us for 266 MB, of it the join 15.  One token over 700: 13.3 us, a chain of
+//    join.  9 rows over 65,000: 77 us for 266 MB, of it the join 11.  One token over 700: 13.3 us, a chain of
 //    dependent loads (lengths, page table, keys, values) in two launches.
 //  - trees: the matrix cores and, about as long, the exponentials between the two products.  16 trees of 64
 //    over 16,000, 64 query heads to 8: 845 us, 640 TFLOP/s where a large matrix product reaches 1,150.
@@ -637,17 +637,17 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
 }
 
 // Joins the partials of the item that is cut by the end of workgroup blockIdx.x's stretch, if one is; a
-// workgroup takes four of its rows: a wavefront each where the parts are few, else one
-// after the other with the parts shared out over groups of D / 4 lanes.
-constexpr int kFewParts = 8;
-template <typename T, int D, int kTiles>
-__global__ __launch_bounds__(kAttendThreads) void asd_attend_join_kernel(AttentionArgs a, const float* partials,
-                                                                         const Cut* cuts) {
-    constexpr int kRows = 16 * kTiles, kPer = D / 64, kCols = D / 4, kGroups = kAttendThreads / kCols;
+// workgroup takes four of its rows.  Few parts are loaded all at once by a wavefront a row; of many, kSplit
+// wavefronts a row take a share each.  Four are launched where there are so few items that they have many parts
+// (64 parts of 36 rows: 11 us, 17 with one); one elsewhere, where most of them would find nothing to do
+// (32 blocks over short caches: 8 us, 14 with four).
+constexpr int kFewParts = 8, kPartsAhead = 16, kJoinRows = 4;
+template <typename T, int D, int kTiles, int kSplit>
+__global__ __launch_bounds__(kJoinRows * kSplit * 64) void asd_attend_join_kernel(AttentionArgs a, const float* partials,
+                                                                                 const Cut* cuts) {
+    constexpr int kRows = 16 * kTiles, kPer = D / 64;
     constexpr int64_t kSize = (int64_t)kRows * (D + 2);
-    __shared__ float factor[kAttendThreads];
-    __shared__ f32x4 sums[kGroups][kCols];
-    __shared__ float box[2][kAttendWaves];
+    __shared__ float sums[kSplit][kJoinRows][D + 2];
     const int lane = threadIdx.x & 63, wave = uniform((int32_t)threadIdx.x >> 6);
     const Cut cut = cuts[blockIdx.x];
     if (cut.parts == 0) return;
@@ -658,10 +658,10 @@ __global__ __launch_bounds__(kAttendThreads) void asd_attend_join_kernel(Attenti
         const int32_t p = m / group;
         return (T*)a.out + ((cut.row + p) * a.num_q_heads + cut.head * group + m - p * group) * D;
     };
+    const int row = (int)blockIdx.y * kJoinRows + (wave & (kJoinRows - 1)), split = wave / kJoinRows;
+    const int32_t m = cut.first + row;
     if (cut.parts <= kFewParts) {
-        const int row = (int)blockIdx.y * kAttendWaves + wave;
-        const int32_t m = cut.first + row;
-        if (m >= cut.pairs) return;
+        if (m >= cut.pairs || split > 0) return;
         float top[kFewParts], o[kPer];
         float best = -INFINITY, total = 0.0f;
 #pragma unroll
@@ -686,53 +686,65 @@ __global__ __launch_bounds__(kAttendThreads) void asd_attend_join_kernel(Attenti
         for (int e = 0; e < kPer; ++e) dst[kPer * lane + e] = (T)(o[e] * over);
         return;
     }
-    const int col = threadIdx.x % kCols, mine = threadIdx.x / kCols;
-    for (int r = 0; r < kAttendWaves; ++r) {
-        const int row = (int)blockIdx.y * kAttendWaves + r;
-        const int32_t m = cut.first + row;
-        if (m >= cut.pairs) return;
-        float best = -INFINITY;
-        for (int j = threadIdx.x; j < cut.parts; j += kAttendThreads)
-            best = fmaxf(best, part(j)[kRows * D + row]);
-        for (int s = 32; s > 0; s >>= 1) best = fmaxf(best, __shfl_xor(best, s));
-        __syncthreads();
-        if (lane == 0) box[0][wave] = best;
-        __syncthreads();
+    float best = -INFINITY, total = 0.0f, o[kPer];
+    const int32_t from = m < cut.pairs ? cut.parts * split / kSplit : 0;
+    const int32_t to = m < cut.pairs ? cut.parts * (split + 1) / kSplit : 0;
+    for (int32_t j = from + lane; j < to; j += 64) best = fmaxf(best, part(j)[kRows * D + row]);
+    for (int s = 32; s > 0; s >>= 1) best = fmaxf(best, __shfl_xor(best, s));
 #pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) best = fmaxf(best, box[0][w]);
-        float total = 0.0f;
-        f32x4 o = {0, 0, 0, 0};
-        for (int j0 = 0; j0 < cut.parts; j0 += kAttendThreads) {
-            const int j = j0 + threadIdx.x, here = min(kAttendThreads, cut.parts - j0);
-            float f = 0.0f;
-            if (j < cut.parts) {
-                const float top = part(j)[kRows * D + row];
-                f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - best);
-                total = fmaf(f, part(j)[kRows * (D + 1) + row], total);
-            }
-            __syncthreads();
-            factor[threadIdx.x] = f;
-            __syncthreads();
-#pragma unroll 4
-            for (int x = mine; x < here; x += kGroups) {
-                const f32x4 y = *(const f32x4*)&part(j0 + x)[row * D + 4 * col];
-                o += y * factor[x];
-            }
+    for (int e = 0; e < kPer; ++e) o[e] = 0.0f;
+    for (int32_t j0 = from; j0 < to; j0 += 64) {
+        const int32_t here = min(64, to - j0);
+        float f = 0.0f;
+        if (lane < here) {
+            const float* x = part(j0 + lane);
+            const float top = x[kRows * D + row];
+            f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - best);
+            total = fmaf(f, x[kRows * (D + 1) + row], total);
         }
-        for (int s = 32; s > 0; s >>= 1) total += __shfl_xor(total, s);
-        if (lane == 0) box[1][wave] = total;
-        sums[mine][col] = o;
-        __syncthreads();
-        if (mine == 0) {
-            total = box[1][0] + box[1][1] + box[1][2] + box[1][3];
+        for (int32_t x = 0; x < here; x += kPartsAhead) {
+            float y[kPartsAhead][kPer];
 #pragma unroll
-            for (int x = 1; x < kGroups; ++x) o += sums[x][col];
-            const float over = best == -INFINITY ? 0.0f : 1.0f / total;
-            T* dst = row_of(m);
+            for (int c = 0; c < kPartsAhead; ++c) {
+                const float* from = part(j0 + min(x + c, here - 1)) + row * D + kPer * lane;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) dst[4 * col + e] = (T)(o[e] * over);
+                for (int e = 0; e < kPer; ++e) y[c][e] = from[e];
+            }
+#pragma unroll
+            for (int c = 0; c < kPartsAhead; ++c) {
+                const float weight = __shfl(f, min(x + c, 63));
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) o[e] = fmaf(weight, x + c < here ? y[c][e] : 0.0f, o[e]);
+            }
         }
     }
+    for (int s = 32; s > 0; s >>= 1) total += __shfl_xor(total, s);
+    float* const mine = &sums[split][wave & (kJoinRows - 1)][0];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) mine[kPer * lane + e] = o[e];
+    if (lane == 0) {
+        mine[D] = best;
+        mine[D + 1] = total;
+    }
+    __syncthreads();
+    if (split > 0 || m >= cut.pairs) return;
+    float all = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < kSplit; ++x) all = fmaxf(all, sums[x][wave][D]);
+    total = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < kSplit; ++x) {
+        const float top = sums[x][wave][D], f = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - all);
+        total = fmaf(f, sums[x][wave][D + 1], total);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] = fmaf(f, sums[x][wave][kPer * lane + e], o[e]);
+    }
+    const float over = all == -INFINITY ? 0.0f : 1.0f / total;
+    T* dst = row_of(m);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) dst[kPer * lane + e] = (T)(o[e] * over);
 }
 
 }  // namespace
@@ -768,8 +780,12 @@ hipError_t attend(const AttentionArgs& a, void* workspace, int64_t wgs, hipStrea
     asd_attend_kernel<T, D, kTiles><<<(unsigned)wgs, kAttendThreads, 0, stream>>>(a, partials, cuts);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
-    asd_attend_join_kernel<T, D, kTiles>
-        <<<dim3((unsigned)wgs, 4 * kTiles), kAttendThreads, 0, stream>>>(a, partials, cuts);
+    const dim3 grid((unsigned)wgs, 16 * kTiles / kJoinRows);
+    const int64_t items = (int64_t)a.b.num_requests * a.b.cache.num_heads;
+    if (2 * kFewParts * items * a.team <= wgs)
+        asd_attend_join_kernel<T, D, kTiles, 4><<<grid, kJoinRows * 4 * 64, 0, stream>>>(a, partials, cuts);
+    else
+        asd_attend_join_kernel<T, D, kTiles, 1><<<grid, kJoinRows * 64, 0, stream>>>(a, partials, cuts);
     return hipGetLastError();
 }
 
