@@ -505,8 +505,8 @@ enum {
  * out_q           [total_rows] rows at out_q + r * out_q_stride; may be q itself,
  *                 with q's stride (each head is read before it is written).
  * q, k, v, out_q and the norm weights are 16-byte aligned and the strides
- * multiples of 8.  No other output may alias an input.  Two requests that name
- * one slot leave either's token there.  Allocates nothing; asynchronous.
+ * multiples of 8.  No other output may alias an input.  Where two requests name
+ * one slot, each of its elements is either's.  Allocates nothing; asynchronous.
  */
 asd_status asd_rope_append(const void *q, const void *k, const void *v, asd_dtype dtype,
                            int64_t q_stride, int64_t k_stride, int64_t v_stride,

@@ -1521,14 +1521,12 @@ hipError_t sample(const SampleArgs& a, const Stats& s, int32_t per_wave, int bit
     return hipGetLastError();
 }
 
-}  // namespace
-
 // The workspace's parts, from `base` on (which may be null to add them up).
-static size_t lay_out(int64_t vocab, int64_t rows, char* base, Stats* s) {
+size_t lay_out(int64_t vocab, int64_t rows, char* base, Stats* s) {
     const size_t n = (size_t)rows, groups = (size_t)most_groups(vocab) * n;
     size_t at = 0;
     const auto part = [&](size_t bytes) {
-        char* const p = base + at;
+        char* const p = (char*)((uintptr_t)base + at);
         at += align256(bytes);
         return p;
     };
@@ -1547,26 +1545,47 @@ static size_t lay_out(int64_t vocab, int64_t rows, char* base, Stats* s) {
     return at;
 }
 
-size_t sample_workspace_bytes(int64_t vocab, int64_t rows, int) {
-    Stats s;
-    return lay_out(vocab, rows, nullptr, &s);
-}
+// Rows of a launch: more are drawn by several, one after the other in the same workspace.
+constexpr int64_t kMostRows = (int64_t)1 << 20;
 
-hipError_t launch_sample(const SampleArgs& a, asd_dtype dtype, void* workspace, int cus, hipStream_t stream) {
+template <int kType> hipError_t sample_rows(const SampleArgs& a, void* workspace, int cus, hipStream_t stream) {
     int bits = 62;
     while (((int64_t)1 << (62 - bits)) < a.vocab) --bits;
     if (bits > 50) bits = 50;
     Stats s;
     lay_out(a.vocab, a.rows, (char*)workspace, &s);
-    const int64_t groups = (int64_t)s.groups * a.rows;
     // groups a wavefront takes: as many as leave eight workgroups to a compute unit, eight at most
-    int64_t per_wave = groups / ((int64_t)cus * 8 * kScanWaves);
+    // (4, 16 and 32 took 1.01, 1.03 and 1.2 times as long for 2,112 rows of 151,936)
+    int64_t per_wave = (int64_t)s.groups * a.rows / ((int64_t)cus * 8 * kScanWaves);
     per_wave = per_wave < 1 ? 1 : per_wave > 8 ? 8 : per_wave;
-    while (a.rows * ((s.groups + per_wave * kScanWaves - 1) / (per_wave * kScanWaves)) >= ((int64_t)1 << 31))
-        per_wave *= 2;
-    if (dtype == ASD_F32) return sample<ASD_F32>(a, s, (int32_t)per_wave, bits, cus, stream);
-    if (dtype == ASD_BF16) return sample<ASD_BF16>(a, s, (int32_t)per_wave, bits, cus, stream);
-    return sample<ASD_F16>(a, s, (int32_t)per_wave, bits, cus, stream);
+    return sample<kType>(a, s, (int32_t)per_wave, bits, cus, stream);
+}
+
+}  // namespace
+
+size_t sample_workspace_bytes(int64_t vocab, int64_t rows, int) {
+    Stats s;
+    return lay_out(vocab, rows < kMostRows ? rows : kMostRows, nullptr, &s);
+}
+
+hipError_t launch_sample(const SampleArgs& a, asd_dtype dtype, void* workspace, int cus, hipStream_t stream) {
+    for (int64_t row = 0; row < a.rows; row += kMostRows) {
+        SampleArgs b = a;
+        b.rows = a.rows - row < kMostRows ? a.rows - row : kMostRows;
+        b.logits = (const char*)a.logits + row * a.row_stride * (dtype == ASD_F32 ? 4 : 2);
+        if (a.temperature) b.temperature += row;
+        if (a.top_k) b.top_k += row;
+        if (a.top_p) b.top_p += row;
+        if (a.min_p) b.min_p += row;
+        b.uniform += row;
+        b.out_token += row;
+        if (a.out_prob) b.out_prob += row;
+        const hipError_t err = dtype == ASD_F32    ? sample_rows<ASD_F32>(b, workspace, cus, stream)
+                               : dtype == ASD_BF16 ? sample_rows<ASD_BF16>(b, workspace, cus, stream)
+                                                   : sample_rows<ASD_F16>(b, workspace, cus, stream);
+        if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
 }
 
 }  // namespace asd

@@ -229,3 +229,23 @@ def test_an_empty_batch_is_a_no_op():
     got = asd.asd_block_attention(queries(b)[:0], b.k_cache, b.v_cache, b.page_table[:0],
                                   b.cache_lens[:0], b.block_lens[:0], out=out)
     assert got.shape == (0, 4, 64)
+
+
+def test_repeated_calls_and_two_streams_give_the_same():
+    b = Batch([8, 0, 40], [30000, 5000, 77], 16, 4, 128, BF16, 16, seed=31)
+    c = Batch([0] * 20, list(range(100, 8100, 400)), 16, 4, 128, BF16, 64, seed=32)
+    calls = []
+    for x in (b, c):
+        q = queries(x)
+        calls.append(lambda x=x, q=q: asd.asd_block_attention(q, x.k_cache, x.v_cache, x.page_table,
+                                                              x.cache_lens, x.block_lens))
+    want = [call() for call in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(6):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(calls[i]())
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want[i]) for i in range(2) for x in got[i])

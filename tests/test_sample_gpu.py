@@ -250,3 +250,54 @@ def test_counts_next_to_the_width(dtype, vocab):
     for p in (1.0, 0.9, 0.3):
         check(z, u, k=k, p=p)
         check(z, u, k=k[::-1], p=p, m=1e-3, t=1.5)
+
+
+def test_more_rows_than_a_launch_takes():
+    """Each row's token is that of the same row in a small batch."""
+    base, vocab, rows = 1000, 40, (1 << 20) + 1234        # rows of 40 binary16 logits keep their alignment
+    z, u = rows_of(base, vocab, torch.float16, 17)
+    gen = torch.Generator().manual_seed(18)
+    u = u.to(DEV)
+    p = torch.rand(base, generator=gen).to(DEV)
+    k = torch.randint(0, 30, (base,), generator=gen).to(torch.int32).to(DEV)
+    want = asd.asd_sample(z, u, top_k=k, top_p=p)
+    many = torch.arange(rows, device=DEV) % base
+    prob = torch.zeros(rows, device=DEV)
+    got = asd.asd_sample(z[many], u[many], top_k=k[many], top_p=p[many], out_prob=prob)
+    assert torch.equal(got, want[many])
+    assert bool((prob > 0).all())
+
+
+def test_repeated_calls_give_the_same():
+    z, u = rows_of(300, 90001, torch.bfloat16, 23)
+    p = torch.full((300,), 0.97, device=DEV)
+    probs = [torch.empty(300, device=DEV) for _ in range(4)]
+    tokens = [asd.asd_sample(z, u.to(DEV), top_p=p, out_prob=x).tolist() for x in probs]
+    assert all(t == tokens[0] for t in tokens) and all(torch.equal(x, probs[0]) for x in probs)
+
+
+@pytest.mark.parametrize("vocab", [500, 5000, 70000])
+def test_temperatures_at_the_ends(vocab):
+    z, u = rows_of(8, vocab, torch.float32, vocab)
+    t = [1e-38, 1e-30, 1e-6, 1e-3, 1e6, 1e30, 3e38, math.inf]
+    check(z, u, t=t)
+    check(z, u, t=t, p=0.6)
+    check(z, u, t=t, k=30, p=0.6, m=0.2)
+    check(z, u, t=t, k=vocab // 2, p=0.6)
+
+
+def test_two_streams_at_once():
+    """Each stream has a library workspace of its own."""
+    z = [rows_of(64, 100000, torch.bfloat16, s) for s in (1, 2)]
+    args = [(x[0], x[1].to(DEV)) for x in z]
+    p = torch.full((64,), 0.95, device=DEV)
+    want = [asd.asd_sample(*a, top_p=p).tolist() for a in args]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(asd.asd_sample(*args[i], top_p=p))
+    torch.cuda.synchronize()
+    assert all(t.tolist() == want[i] for i in range(2) for t in got[i])
