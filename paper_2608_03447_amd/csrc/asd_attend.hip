@@ -24,7 +24,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 // Bounds and measurements (128-element heads in bfloat16, 32 query heads to 8 key heads unless said):
 //  - single tokens and blocks: the cache's bytes.  64 single tokens over up to 8,192: 218 us, 4.9 TB/s where a
 //    plain read reaches 6.9; some 25 us of it are the batch's sharing out, each item's first loads and the
-//    join.  9 rows over 65,000: 76 us for 266 MB, of it the join 11.  One token over 700: 13.4 us, a chain of
+//    join.  9 rows over 65,000: 76 us for 266 MB, of it the join 11.  One token over 700: 12.7 us, a chain of
 //    dependent loads (lengths, page table, keys, values) in two launches.
 //  - trees: the matrix cores and, about as long, the exponentials between the two products.  16 trees of 64
 //    over 16,000, 64 query heads to 8: 839 us, 640 TFLOP/s where a large matrix product reaches 1,150.
@@ -101,6 +101,54 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* box, int64_t* 
     return before + sum - v;
 }
 
+// Equal stretches, the last one short.  Workgroups go to the XCDs in turn; those of a stretch,
+// which read the same keys and values, go to one of them, and so do neighbouring stretches.
+struct Shares {
+    int64_t per;
+    int32_t worker;     // -1: this workgroup has none
+    __device__ __forceinline__ Shares(int64_t total, int32_t team) {
+        const int64_t most = gridDim.x / team;
+        per = total <= most ? 1 : quotient(total + most - 1, most);
+        const int32_t used = (int32_t)(per == 1 ? total : quotient(total + per - 1, per)) * team;
+        const int32_t eighth = (used + 7) / 8, at = (int32_t)(blockIdx.x >> 3);
+        worker = (int32_t)(blockIdx.x & 7) * eighth + at;
+        if (at >= eighth || worker >= used) worker = -1;
+    }
+};
+
+// The same for up to 64 requests, every wavefront for itself, a lane a request: no barrier (1.2 us of a call).
+template <int kRows>
+__device__ __forceinline__ Where locate_few(const Blocks& b, int32_t group, int32_t team) {
+    const int32_t n = b.num_requests, lane = threadIdx.x & 63;
+    const bool in = lane < n;
+    const int32_t k = in ? b.block_lens[lane] : 0, count = rows_of_block(k);
+    const int64_t cached = in ? b.cache_lens[lane] : 0;
+    const auto scan = [&](long long x) {
+        for (int s = 1; s < n; s <<= 1) {
+            const long long up = __shfl_up(x, s);
+            if (lane >= s) x += up;
+        }
+        return (int64_t)x;
+    };
+    int64_t row = 0;
+    if (b.row_offsets)
+        row = in ? b.row_offsets[lane] : 0;
+    else if (n > 1)
+        row = scan(in ? count : 0) - count;
+    uint32_t err = k < 0 ? kDecodeErrNegativeK : 0u;
+    const int64_t units = in ? units_of<kRows>(b, group, team, row, count, cached, err) : 0;
+    if (blockIdx.x == 0 && threadIdx.x < 64 && err != 0) atomicOr(b.error_word, err);
+    const int64_t upto = scan(units), total = uniform((int64_t)__shfl((long long)upto, n - 1));
+    const Shares shares(total, team);
+    if (shares.worker < 0) return Where{-1, 0, 0, 0, 0, 0, 0, 0, 0};
+    const int32_t id = shares.worker / team;
+    const int64_t unit = id * shares.per;
+    const int at = __builtin_ctzll(__ballot(in && unit < upto));
+    const auto of = [&](int64_t x) { return uniform((int64_t)__shfl((long long)x, at)); };
+    return Where{id,          shares.worker - id * team, shares.per, total, unit - of(upto - units), of(row),
+                 of(cached), at,                        uniform(__shfl(count, at))};
+}
+
 // The workgroup's stretch: every thread sums its share of the requests (one, up to 256 requests),
 // and the one whose share holds the stretch's first unit says where it is.
 template <int kRows>
@@ -126,14 +174,10 @@ __device__ __forceinline__ Where locate(const Blocks& b, int32_t group, int32_t 
     if (blockIdx.x == 0 && err != 0) atomicOr(b.error_word, err);
     int64_t total;
     int64_t before = block_scan(units, box, &total);
-    // Equal stretches, the last one short.  Workgroups go to the XCDs in turn; those of a stretch,
-    // which read the same keys and values, go to one of them, and so do neighbouring stretches.
-    const int64_t most = gridDim.x / team, per = total <= most ? 1 : quotient(total + most - 1, most);
-    const int32_t used = (int32_t)(per == 1 ? total : quotient(total + per - 1, per)) * team, eighth = (used + 7) / 8;
-    const int32_t worker = (int32_t)(blockIdx.x & 7) * eighth + (int32_t)(blockIdx.x >> 3);
-    if ((int32_t)(blockIdx.x >> 3) >= eighth || worker >= used) return Where{-1, 0, 0, 0, 0, 0, 0, 0, 0};
-    const int32_t id = worker / team;
-    const int64_t unit = id * per;
+    const Shares shares(total, team);
+    if (shares.worker < 0) return Where{-1, 0, 0, 0, 0, 0, 0, 0, 0};
+    const int32_t worker = shares.worker, id = worker / team;
+    const int64_t per = shares.per, unit = id * per;
     if (unit >= before && unit < before + units) {
         for (int32_t i = first; i < last; ++i) {
             const int32_t count = rows_of_block(i == first ? k0 : b.block_lens[i]);
@@ -243,7 +287,8 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
 
     const asd_paged_cache& cache = a.b.cache;
     const int32_t group = a.num_q_heads / cache.num_heads;
-    Where at = locate<kRows>(a.b, group, a.team, box, &where_box);
+    Where at = a.b.num_requests <= 64 ? locate_few<kRows>(a.b, group, a.team)
+                                      : locate<kRows>(a.b, group, a.team, box, &where_box);
     if (at.id < 0) {
         if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{0, 0, 0, 0, 0, 0};
         return;
@@ -271,7 +316,7 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
         }
         const int32_t pairs = count * group, tiles = (pairs + kRows - 1) / kRows;
         const int64_t units = (cached64 + count + kUnit - 1) / kUnit;
-        const int64_t item = quotient(at.unit, units), from = at.unit - item * units;
+        const int64_t item = at.unit < units ? 0 : quotient(at.unit, units), from = at.unit - item * units;
         const int64_t to = from + left < units ? from + left : units;
         const int32_t rounds = (tiles + a.team - 1) / a.team, head = (int32_t)item / rounds;
         const int32_t mine = ((int32_t)item - head * rounds) * a.team + at.member, first = mine * kRows;      // of the pairs
