@@ -905,8 +905,8 @@ struct Units {
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPartList = 1024;
 
 // Whether rows are shared out: where pass 2 can hold their sub-blocks, and they are long, or many, enough to
-// pay for three more launches, 6 us where no row is flat.  One flat row of 32,000 takes 83 us alone, one of
-// 65,000 111 us, one of 151,936 55 us shared out; 300 of 32,000 take 120 us alone.
+// pay for three more launches, 6 us where no row is flat.  One flat row of 32,000 takes 63 us alone, one of
+// 65,000 96 us, one of 151,936 56 us shared out, and so do 16 of 32,000 in 46.
 bool shares_out(int64_t vocab, int64_t rows) {
     return vocab > (rows < 8 ? 65536 : 8192) && vocab + 7 <= (int64_t)kMostSubs * kSub;
 }
@@ -1147,11 +1147,13 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleA
 
 // ------------------------------------------------------------ pass 6
 
-constexpr int kFlatThreads = 1024, kFlatWaves = kFlatThreads / 64, kBins = 4096, kCollected = 8192, kSpans = 1024;
+constexpr int kFlatThreads = 512, kFlatWaves = kFlatThreads / 64, kBins = 4096, kCollected = 8192, kSpans = kFlatThreads;
 
 // A whole row by one workgroup: histograms of it give the bin that holds the cut, a second reading lists that bin
-// and sums what lies above it.  Each reading of 129,280 logits takes 50 us, the exponentials' time on one
-// compute unit.  Spans (1,024 tokens each up to 2^20 tokens a row) hold what is kept of them.
+// and sums what lies above it.  Each reading is the exponentials' time on one compute unit, some 40 us for
+// 129,280 logits.  Spans (1,024 tokens each up to 2^19 tokens a row) hold what is kept of them.  512
+// threads: 1,024, whose registers did not hold everything, took 61 us against 38 for a call of 8,000 logits with
+// top-p, 83 against 63 for one of 32,000.
 template <int kType>
 __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, int bits, int64_t row) {
     typedef typename Element<kType>::T T;
@@ -1237,12 +1239,13 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
     };
     // The bin in which `want` is reached, from the last one down, and what is still wanted of it: four bins a thread.
     const auto find_bin = [&](bool weights, u64* want) -> uint32_t {
-        u64 four[4], mine = 0, total;
+        constexpr int kEach = kBins / kFlatThreads;
+        u64 each[kEach], mine = 0, total;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int b = kBins - 1 - (4 * tid + i);
-            four[i] = weights ? bin_weight[b] : bin_count[b];
-            mine += four[i];
+        for (int i = 0; i < kEach; ++i) {
+            const int b = kBins - 1 - (kEach * tid + i);
+            each[i] = weights ? bin_weight[b] : bin_count[b];
+            mine += each[i];
         }
         u64 have = block.before(mine, block.u, &total);
         if (tid == 0) {
@@ -1251,13 +1254,13 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
         }
         __syncthreads();
         if (have < *want && have + mine >= *want) {
-            for (int i = 0; i < 4; ++i) {
-                if (have + four[i] >= *want) {
-                    pick[0] = (u64)(kBins - 1 - (4 * tid + i));
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                if (have < *want && have + each[i] >= *want) {
+                    pick[0] = (u64)(kBins - 1 - (kEach * tid + i));
                     pick[1] = *want - have;
-                    break;
                 }
-                have += four[i];
+                have += each[i];
             }
         }
         __syncthreads();
