@@ -441,7 +441,8 @@ asd_status asd_lmhead_verify(const void *hidden, const void *weight, int64_t d, 
  * is skipped (ASD_DEVERR_ROWS), and so is one with cache_len_i < 0 or
  * cache_len_i + K_i + 1 > max_pages * page_size (ASD_DEVERR_CACHE): none of its
  * rows, and none of its tokens in the cache, is written.  Rows that no request
- * owns are left as they were.
+ * owns are left as they were; a row that two requests own holds elements of either's
+ * result, so with out_q = q no row may have two owners.
  */
 
 /*
