@@ -531,8 +531,8 @@ asd_status asd_rope_append(const void *q, const void *k, const void *v, asd_dtyp
  * What hidden tokens hold, infinities and NaN too, does not reach the row.
  *
  * Scores, maxima, sums and outputs are held in binary32, the weights enter the
- * second product rounded to dtype (as the matrix cores take them) and the
- * output is rounded once.  The same call gives the same bits; where a sequence is
+ * second product and their sum rounded to dtype (as the matrix cores take them)
+ * and the output is rounded once.  The same call gives the same bits; where a sequence is
  * cut for the chip's workgroups depends on the batch, and with it a row's last bits.
  *
  * q               row r's heads, dense, at q + r * q_stride (elements, a multiple
