@@ -23,7 +23,7 @@ LIBRARY = os.path.join(HERE, "libasd.so")
 # The decoding operators around the verifier, and the header they share.
 DECODE_SOURCES = [os.path.join(CSRC, "asd_decode_api.cpp"), os.path.join(CSRC, "asd_cache.hip"),
                   os.path.join(CSRC, "asd_attend.hip"), os.path.join(CSRC, "asd_sample.hip")]
-DECODE_HEADERS = [os.path.join(CSRC, "asd_decode.h")]
+DECODE_HEADERS = [os.path.join(CSRC, "asd_decode.h"), os.path.join(CSRC, "asd_tokens.h")]
 SOURCES = [os.path.join(CSRC, "asd_api.cpp"), os.path.join(CSRC, "asd_kernels.hip"), *DECODE_SOURCES]
 # The verifier's sources and headers; with DECODE_SOURCES and DECODE_HEADERS, every file whose
 # code goes into the library.

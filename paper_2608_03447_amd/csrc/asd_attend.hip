@@ -3,6 +3,7 @@
 #include <stdint.h>
 
 #include "asd_decode.h"
+#include "asd_tokens.h"
 
 namespace asd {
 namespace {
@@ -30,9 +31,7 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 //    over 16,000, 64 query heads to 8: 839-871 us, 620-640 TFLOP/s where a large matrix product reaches 1,150.
 // A kernel of a workgroup per (row, head), one token at a time, took 13,309, 56,835, 466 and 476,524 us.
 
-constexpr int kAttendThreads = 256, kAttendWaves = kAttendThreads / 64;
-constexpr int kStrip = 32;                          // tokens a wavefront takes at a time
-constexpr int kUnit = kStrip * kAttendWaves;
+constexpr int kAttendThreads = 64 * kAttendWaves;
 constexpr int32_t kMostTeam = 32;
 
 // The same value in every lane, in scalar registers.
@@ -377,11 +376,12 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
             sum[tile] = 0.0f;
         }
         // a chain's rows see no token behind the tile's last one
-        const int32_t cached = (int32_t)cached64, end_all = cached + count;
+        const int32_t cached = (int32_t)cached64;
+        const Tokens tokens{(Token)(cached + count), (uint32_t)cache.page_size, a.page_magic, a.page_shift};
         const int32_t last_p = uniform(row_p[kRows - 1]);
-        const int32_t end = a.mask ? end_all : cached + last_p + 1;
-        const int32_t strip_end = (int32_t)min(to * kUnit, (int64_t)end);
-        int32_t strip = (int32_t)(from * kUnit) + wave * kStrip;
+        const int32_t end = a.mask ? (int32_t)tokens.end : cached + last_p + 1;
+        const Token strip_end = (Token)min(to * kUnit, (int64_t)end);
+        Token strip = (Token)(from * kUnit) + wave * kStrip;
         const int32_t* const table = cache.page_table + (int64_t)at.request * cache.max_pages;
         const char* const keys = (const char*)((const T*)cache.keys + (int64_t)head * cache.head_stride ); 
         const char* const values = (const char*)((const T*)cache.values + (int64_t)head * cache.head_stride + NC * n);
@@ -389,13 +389,11 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
         // A strip's page ids (lanes l and l + 32 hold token l; tokens behind the last one take
         // its page) and, from them, its tokens' byte offsets in LDS; the mask of the tokens that
         // are there, the others' offsets being 0.
-        const auto page_at = [&](int32_t t) { return (int32_t)(__umulhi(2 * (uint32_t)t, a.page_magic) >> a.page_shift); };
-        const auto page_of = [&](int32_t t0) -> int32_t { return table[page_at(min(t0 + (lane & 31), end_all - 1))]; };
-        const auto put_offsets = [&](int b, int32_t t0, int32_t page) -> uint32_t {
-            const int32_t t = t0 + (lane & 31);
-            const bool ok = t < end_all && (uint32_t)page < (uint32_t)cache.num_pages;
-            const int32_t slot = t - page_at(t) * cache.page_size;
-            const int64_t off = ((int64_t)page * cache.page_stride + (int64_t)slot * cache.token_stride) * 2;
+        const auto page_of = [&](Token t0) -> int32_t { return table[tokens.entry(t0 + (lane & 31))]; };
+        const auto put_offsets = [&](int b, Token t0, int32_t page) -> uint32_t {
+            const Token t = t0 + (lane & 31);
+            const bool ok = tokens.has(t) && (uint32_t)page < (uint32_t)cache.num_pages;
+            const int64_t off = ((int64_t)page * cache.page_stride + (int64_t)tokens.slot(t) * cache.token_stride) * 2;
             wave_sync();
             if (lane < 32) offsets[wave][b][lane] = ok ? off : 0;
             wave_sync();
@@ -526,7 +524,7 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
             asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kStrip / kAtOnce + 8 * kVecs) : "memory");
         }
         // Strips that every row sees whole.
-        while (strip < strip_end && valid == ~0u && strip + kStrip <= cached) {
+        while (strip < strip_end && valid == ~0u && strip + kStrip <= (Token)cached) {
             const int32_t after = page_of(strip + 2 * kUnit);
             weigh(b, true, 0);
             add_values();
@@ -541,11 +539,11 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
         // The others: the block's own tokens, the strip that the sequence ends in, bad pages.
 #pragma unroll 1
         while (strip < strip_end) {
-            if (lane < 32 && strip + lane < end_all && !((valid >> lane) & 1))
+            if (lane < 32 && tokens.has(strip + lane) && !((valid >> lane) & 1))
                 atomicOr(a.b.error_word, kDecodeErrCache);
             // the tokens that each tile's row sees, a bit each: cached ones, and the block's by the mask
             uint32_t window[kTiles];
-            const int32_t past = strip - cached;         // the block's first token; negative: before it
+            const int32_t past = (int32_t)strip - cached;         // the block's first token; negative: before it
 #pragma unroll
             for (int tile = 0; tile < kTiles; ++tile) {
                 const int32_t p = row_p[16 * tile + n];
@@ -558,7 +556,7 @@ __global__ __launch_bounds__(kAttendThreads, resident(D, kTiles)) void asd_atten
                     const int32_t before = min(max(-past, 0), 32);
                     window[tile] = (uint32_t)(bits << before) | (uint32_t)((1ull << before) - 1);
                 } else {
-                    window[tile] = (uint32_t)((1ull << min(max(p + 1 - past, 0), 32)) - 1);
+                    window[tile] = (uint32_t)((1ull << chain_sees(p, past)) - 1);
                 }
             }
             // of the lane's 8 tokens: which its rows see, 8 bits a tile, and which are there at all
@@ -883,9 +881,7 @@ hipError_t launch_block_attention(const AttentionArgs& a, bool bf16, void* works
                                   hipStream_t stream) {
     const asd_paged_cache& c = a.b.cache;
     AttentionArgs b = a;
-    b.page_shift = 0;
-    while (((int64_t)1 << b.page_shift) < c.page_size) ++b.page_shift;
-    b.page_magic = (uint32_t)((((uint64_t)1 << (31 + b.page_shift)) + c.page_size - 1) / c.page_size);
+    page_divisor(c.page_size, &b.page_magic, &b.page_shift);
     const int tiles = tiles_of(a.num_q_heads, c.num_heads, c.head_dim, a.b.num_requests, a.b.total_rows);
     const int64_t wgs = (int64_t)cus * resident(c.head_dim, tiles);
     b.team = team_of(a.num_q_heads, c.num_heads, a.b.num_requests, a.b.total_rows, tiles);

@@ -68,9 +68,7 @@ struct AttentionArgs {
     const uint64_t* mask;
     int32_t mask_words;
     void* out;
-    // t / page_size = (2 t page_magic / 2^32) >> page_shift for 0 <= t < 2^31: with 2^shift >=
-    // page_size and magic = ceil(2^(31 + shift) / page_size) the excess stays below 1 / page_size.
-    uint32_t page_magic;
+    uint32_t page_magic;   // of Tokens
     int32_t page_shift;
     int32_t team;          // workgroups that share a stretch
 };
