@@ -259,7 +259,8 @@ __device__ __forceinline__ float rows_sum(float x) {
 
 // Weights are exp2 of scores less a reference that trails the greatest one: they reach 2^kLead
 // at most, and the reference is moved, and what was summed rescaled, only when one would pass that.
-// Then the greatest is put at 2^kSet, which keeps weights down to 2^-30 of it normal in binary16.
+// Then the greatest is put at 2^kSet, which keeps weights down to 2^-20 of it normal in binary16 and those down to
+// 2^-30 subnormal, rounded by 2^-31 of it at most.
 constexpr float kLead = 14.0f, kSet = 6.0f;
 
 // One workgroup per stretch.  Every wavefront walks strips of 32 tokens of its
