@@ -539,7 +539,7 @@ asd_status asd_rope_append(const void *q, const void *k, const void *v, asd_dtyp
  *                 of 8); dtype ASD_BF16 or ASD_F16; 16-byte aligned.
  * num_q_heads     a positive multiple of cache->num_heads, at most 65,536; times
  *                 total_rows below 2^31.
- * scale           finite.
+ * scale           finite, 2^127 in size at most.
  * cache           head_dim 64, 128 or 256.
  * mask            uint64 [total_rows][mask_words], or NULL with mask_words = 0.
  * out             [total_rows][num_q_heads][head_dim], dense, 16-byte aligned; no

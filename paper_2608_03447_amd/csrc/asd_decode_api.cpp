@@ -141,7 +141,8 @@ asd_status asd_block_attention(const void* q, asd_dtype dtype, int64_t q_stride,
     if (st != ASD_OK) return st;
     if (!cache || bad_batch(num_requests, total_rows) || bad_cache(*cache, num_requests))
         return ASD_EINVAL;
-    if (bad_heads(num_q_heads, cache->num_heads, cache->head_dim) || !std::isfinite(scale))
+    // (scale log2(e) has to be finite)
+    if (bad_heads(num_q_heads, cache->num_heads, cache->head_dim) || !(std::fabs(scale) <= 0x1p127f))
         return ASD_EINVAL;
     if (total_rows * num_q_heads >= k2G) return ASD_EINVAL;
     if (mask_words < 0 || (mask != nullptr) != (mask_words > 0)) return ASD_EINVAL;
