@@ -527,7 +527,8 @@ asd_status asd_rope_append(const void *q, const void *k, const void *v, asd_dtyp
  * over the tokens t < cache_len_i + K_i + 1 that the row sees: every cached one
  * (t < cache_len_i), and the block's token j = t - cache_len_i where bit j mod 64
  * of mask[r][j / 64] is set (j >= 64 * mask_words: not seen); with a NULL mask the
- * tokens j <= p (a chain of drafts).  A row that sees nothing gives zeros.
+ * tokens j <= p (a chain of drafts).  A row that sees nothing, or no score above
+ * -infinity, gives zeros.
  * What hidden tokens hold, infinities and NaN too, does not reach the row.
  *
  * Scores, maxima, sums and outputs are held in binary32, the weights enter the
