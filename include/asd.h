@@ -579,10 +579,11 @@ size_t asd_block_attention_workspace_bytes(int32_t num_q_heads, int32_t num_kv_h
  * and the token drawn is the first, by index, at which the running sum of the
  * kept weights exceeds u times their sum.  T <= 0 or NaN: the row's argmax
  * (lowest index among equals), whatever k, p, min_p and u are.  Weights are
- * held to 2^-44 of the greatest or better and summed in binary64 or as integers, in an order
- * that depends on the row alone and on its address modulo 16: a token is the one
- * above unless u, or a cut, lies within 2^-40 of an edge, and a call's other rows
- * have no part in it.
+ * computed in binary64, to 2^-44 of themselves from 2^-64 of the greatest on, and
+ * summed in binary64 or as whole numbers of 2^-64 of the greatest, in an order that
+ * depends on the row, its address modulo 16 and whether the call has 8 rows: a
+ * token is the one above unless u, or a cut, lies within 2^-40 of the mass of an
+ * edge (beyond 2^24 logits, within vocab 2^-64).
  *
  * -0 equals +0; a logit of -inf has no weight; where the greatest is +inf the
  * tokens at +inf share the weight.  A row that holds a NaN, or nothing but -inf,

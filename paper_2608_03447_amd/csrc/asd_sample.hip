@@ -13,10 +13,12 @@
 // are found among the candidates, up to 2,048, by their order.
 //
 // Rows that keep more tokens than that (a nucleus of tens of thousands) are read again in parts by all workgroups: pass
-// 3 sums their weights by bins of the logit, pass 4 lists the tokens of the bin that holds the cut and sums, group by
-// group, what lies above it, and pass 5 (finish) finds the cut among the listed and draws.  Pass 6 (flat), one
+// 3 sums their weights, coarsely, by bins of the logit, pass 4 lists the tokens of the bin that holds the cut and sums,
+// group by group, what lies above it, and pass 5 (finish) finds the cut among the listed and draws.  Pass 6 (flat), one
 // workgroup a row, takes what is left: calls too small for passes 3 to 5, top-k beyond 1,920, bins of more
-// ties than a list holds.
+// ties than a list holds, cuts that the coarse sums put into another bin than the exact ones.
+//
+// A sum in a fixed order is binary64; one whose order the hardware chooses is of whole numbers (Mass, Coarse).
 //
 // Bounds and measurements: pass 1 is memory's and the binary64 exponentials'; 2,112 rows of 151,936 float32
 // (1.28 GB) take 267 us, 4.8 TB/s.  Pass 2 is latency and, with 1,400 candidates, arithmetic: 12 us for
@@ -97,6 +99,38 @@ struct Weights {
     }
 };
 
+// A sum of weights in whole numbers of 2^-64 of the greatest, so that it is the same in any order: `high` counts
+// 2^-32 and `low`, which has a sign, 2^-64.  A weight adds 2^32 and 2^31 at most, so that the sums of 2^30 fit.
+typedef unsigned __int128 u128;
+struct Mass {
+    u64 high, low;
+    __device__ __forceinline__ Mass operator+(const Mass& o) const { return {high + o.high, low + o.low}; }
+    __device__ __forceinline__ Mass operator-(const Mass& o) const { return {high - o.high, low - o.low}; }
+    __device__ __forceinline__ Mass operator*(u64 n) const { return {high * n, low * n}; }
+    __device__ __forceinline__ void operator+=(const Mass& o) { *this = *this + o; }
+    __device__ __forceinline__ u128 value() const { return ((u128)high << 32) + (u128)(__int128)(long long)low; }
+};
+// A weight added to 2^20 is rounded to a multiple of 2^-32, which then stands in the sum's low bits; what it was
+// rounded by, exact, gives the rest the same way.
+__device__ __forceinline__ Mass mass_of(double weight) {
+    constexpr double kHigh = 0x1p20, kLow = 0x1.8p-12;
+    const double t = weight + kHigh, r = (weight - (t - kHigh)) + kLow;
+    return {__builtin_bit_cast(u64, t) - __builtin_bit_cast(u64, kHigh),
+            __builtin_bit_cast(u64, r) - __builtin_bit_cast(u64, kLow)};
+}
+__device__ __forceinline__ double real_of(u128 units) {
+    return (double)(u64)(units >> 32) * 0x1p-32 + (double)(uint32_t)units * 0x1p-64;
+}
+// ceil(x 2^64) for 0 <= x < 2^30.
+__device__ __forceinline__ u128 units_of(double x) {
+    const double high = floor(x * 0x1p32);
+    return ((u128)(u64)high << 32) + (u64)ceil((x * 0x1p32 - high) * 0x1p32);
+}
+__device__ __forceinline__ void add_to(u64* high, u64* low, const Mass& m) {
+    atomicAdd(high, m.high);
+    atomicAdd(low, m.low);
+}
+
 // Row parameters.
 struct Row {
     float t, p, m;
@@ -124,7 +158,8 @@ struct Near {
     float high, steps;     // steps: bins to a unit of the logit
     uint32_t top;          // key of the greatest logit
     uint32_t collected;    // tokens of the cut's bin that pass 4 listed, in the place of the row's sub-blocks
-    u64 rest;              // mass that is wanted of them
+    double all;            // the row's mass
+    Mass above;            // of the tokens above that bin
     __device__ __forceinline__ uint32_t bin(float x) const {
         return (uint32_t)(kNearBins - 1) - (uint32_t)fminf(fmaxf((high - x) * steps, 0.0f), (float)(kNearBins - 1));
     }
@@ -362,10 +397,50 @@ __global__ __launch_bounds__(kScanThreads) void asd_sample_scan_kernel(SampleArg
 
 // ------------------------------------------------------------ workgroup sums
 
+// The same for masses, and the sum over the lanes up to each one.
+template <int kCtrl, int kRows = 0xf>
+__device__ __forceinline__ u64 dpp(u64 x) {
+    const u32x2 u = __builtin_bit_cast(u32x2, x);
+    return __builtin_bit_cast(u64, u32x2{(uint32_t)__builtin_amdgcn_update_dpp(0, (int)u.x, kCtrl, kRows, 0xf, false),
+                                         (uint32_t)__builtin_amdgcn_update_dpp(0, (int)u.y, kCtrl, kRows, 0xf, false)});
+}
+__device__ __forceinline__ u64 wave_sum(u64 x) {
+    x += dpp<kXor1>(x);
+    x += dpp<kXor2>(x);
+    x += dpp<kHalfMirror>(x);
+    x += dpp<kMirror>(x);
+    u32x2 u = __builtin_bit_cast(u32x2, x);
+    u32x2 a = __builtin_amdgcn_permlane16_swap(u.x, u.x, false, false);
+    u32x2 b = __builtin_amdgcn_permlane16_swap(u.y, u.y, false, false);
+    u = __builtin_bit_cast(u32x2, __builtin_bit_cast(u64, u32x2{a.x, b.x}) + __builtin_bit_cast(u64, u32x2{a.y, b.y}));
+    a = __builtin_amdgcn_permlane32_swap(u.x, u.x, false, false);
+    b = __builtin_amdgcn_permlane32_swap(u.y, u.y, false, false);
+    return __builtin_bit_cast(u64, u32x2{a.x, b.x}) + __builtin_bit_cast(u64, u32x2{a.y, b.y});
+}
+__device__ __forceinline__ u64 wave_scan(u64 x) {
+    constexpr int kUp = 0x110, kLast15 = 0x142, kLast31 = 0x143;
+    x += dpp<kUp + 1>(x);
+    x += dpp<kUp + 2>(x);
+    x += dpp<kUp + 4>(x);
+    x += dpp<kUp + 8>(x);
+    x += dpp<kLast15, 0xa>(x);
+    return x + dpp<kLast31, 0xc>(x);
+}
+__device__ __forceinline__ Mass wave_sum(const Mass& m) { return {wave_sum(m.high), wave_sum(m.low)}; }
+__device__ __forceinline__ Mass wave_scan(const Mass& m) { return {wave_scan(m.high), wave_scan(m.low)}; }
+template <typename V> __device__ __forceinline__ V wave_scan(V run) {
+    for (int x = 1; x < 64; x <<= 1) {
+        const V up = __shfl_up(run, x);
+        if ((int)(threadIdx.x & 63) >= x) run += up;
+    }
+    return run;
+}
+
 template <int kN> struct Block {
     static constexpr int kWaves = kN / 64;
     double d[kWaves];
     u64 u[kWaves];
+    Mass m[kWaves];
 
     __device__ __forceinline__ uint32_t max(uint32_t v) {
         for (int x = 32; x > 0; x >>= 1) v = ::max(v, (uint32_t)__shfl_xor((int)v, x));
@@ -376,6 +451,14 @@ template <int kN> struct Block {
         return v;
     }
     __device__ __forceinline__ uint32_t min(uint32_t v) { return ~max(~v); }
+    __device__ __forceinline__ uint32_t any(uint32_t v) {
+        for (int x = 32; x > 0; x >>= 1) v |= (uint32_t)__shfl_xor((int)v, x);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) u[threadIdx.x >> 6] = v;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) v |= (uint32_t)u[w];
+        return v;
+    }
     __device__ __forceinline__ uint32_t count(uint32_t v) {
         for (int x = 32; x > 0; x >>= 1) v += (uint32_t)__shfl_xor((int)v, x);
         __syncthreads();
@@ -394,13 +477,13 @@ template <int kN> struct Block {
         for (int w = 0; w < kWaves; ++w) all += d[w];
         return all;
     }
-    __device__ __forceinline__ u64 sum(u64 v) {
-        for (int x = 32; x > 0; x >>= 1) v += (u64)__shfl_xor((long long)v, x);
+    __device__ __forceinline__ Mass sum(Mass v) {
+        v = wave_sum(v);
         __syncthreads();
-        if ((threadIdx.x & 63) == 0) u[threadIdx.x >> 6] = v;
+        if ((threadIdx.x & 63) == 0) m[threadIdx.x >> 6] = v;
         __syncthreads();
-        u64 all = 0;
-        for (int w = 0; w < kWaves; ++w) all += u[w];
+        Mass all{0, 0};
+        for (int w = 0; w < kWaves; ++w) all += m[w];
         return all;
     }
     // The sum of a number that each wavefront has, with one barrier: the place alternates with `turn`, which the
@@ -418,15 +501,11 @@ template <int kN> struct Block {
     template <typename V>
     __device__ __forceinline__ V before(V v, V* box, V* total) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        V run = v;
-        for (int x = 1; x < 64; x <<= 1) {
-            const V up = __shfl_up(run, x);
-            if (lane >= x) run += up;
-        }
+        const V run = wave_scan(v);
         __syncthreads();
         if (lane == 63) box[wave] = run;
         __syncthreads();
-        V mine = 0, all = 0;
+        V mine{}, all{};
         for (int w = 0; w < kWaves; ++w) {
             if (w < wave) mine += box[w];
             all += box[w];
@@ -737,7 +816,7 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
             for (int b = tid; b < kNearBins; b += kPickThreads) s.bins[row * kNearBins + b] = 0;
             if (tid == 0) {
                 const float high = value_of(least), range = 4.0f * (high - value_of(low));
-                s.near[row] = Near{high, range > 0.0f ? kNearBins / range : 0.0f, top, 0, 0};
+                s.near[row] = Near{high, range > 0.0f ? kNearBins / range : 0.0f, top, 0, all, Mass{0, 0}};
             }
         }
         if (tid == 0) enqueue(s, shared ? kShared : kAlone, row);
@@ -871,37 +950,51 @@ __global__ __launch_bounds__(kPickThreads) void asd_sample_pick_kernel(SampleArg
 
 // ------------------------------------------------------------ whole rows
 
-// ceil and floor of f * total for a float 0 <= f < 1 and an integer below 2^63, exactly.
-__device__ __forceinline__ u64 share(float f, u64 total, bool up) {
+// ceil and floor of f * total for a float 0 <= f < 1 and a whole number below 2^95, exactly.
+__device__ __forceinline__ u128 share(float f, u128 total, bool up) {
     if (!(f > 0.0f)) return 0;
     int e;
     const uint32_t m = (uint32_t)ldexpf(frexpf(f, &e), 24);   // f = m 2^(e - 24)
     const int shift = 24 - e;
-    const unsigned __int128 x = (unsigned __int128)total * m;
+    const u128 x = total * m;
     if (shift >= 120) return up && x != 0;
-    return (u64)((x + (up ? ((unsigned __int128)1 << shift) - 1 : 0)) >> shift);
+    return (x + (up ? ((u128)1 << shift) - 1 : 0)) >> shift;
 }
 
-// Weights as whole numbers of 2^-bits of the greatest, so that their sum is the same in any order: added to
-// 2^(52 - bits) a weight is rounded to one, which then stands in the sum's low bits.  (A weight below half a
-// unit gives 0, as -inf does.)
-struct Units {
+// Coarse whole numbers, of 2^-bits of the greatest weight, for bins: a row's sum of them fits 62 bits.  What they
+// say of a cut's place is checked by exact sums.
+struct Coarse {
+    double carrier;                 // as in mass_of; a weight below half a unit gives 0
+    __device__ __forceinline__ explicit Coarse(int bits) : carrier((double)(1ull << (52 - bits))) {}
+    __device__ __forceinline__ u64 operator()(double weight) const {
+        return __builtin_bit_cast(u64, weight + carrier) - __builtin_bit_cast(u64, carrier);
+    }
+};
+
+// The fewest tokens of `one` unit each, one at least, that make up `want`.
+__device__ __forceinline__ u64 ties_for(u128 want, u128 one) {
+    u64 n = 0;
+    for (int bit = 30; bit >= 0; --bit)
+        if (one * (n | 1ull << bit) < want) n |= 1ull << bit;
+    return one > 0 ? n + 1 : 1;
+}
+
+// A row's weights.  Where the greatest logit is finite no token needs care: -inf gives 2^-1000, which is no unit.
+struct Reals {
     Weights w;
-    double carrier;
-    bool finite;                    // the greatest logit: then no token needs care
-    __device__ __forceinline__ Units(const Weights& w, int bits, uint32_t top)
-        : w(w), carrier((double)(1ull << (52 - bits))), finite(top < kKeyInf) {}
-    __device__ __forceinline__ u64 operator()(float z) const {
-        const double x = finite ? power2_clamped(((double)z - w.top) * w.per) : w(z);
-        return __builtin_bit_cast(u64, x + carrier) - __builtin_bit_cast(u64, carrier);
+    bool finite;
+    __device__ __forceinline__ Reals(const Weights& w, uint32_t top) : w(w), finite(top < kKeyInf) {}
+    __device__ __forceinline__ double operator()(float z) const {
+        return finite ? power2_clamped(((double)z - w.top) * w.per) : w(z);
     }
 };
 
 // ------------------------------------------------------------ passes 3 and 4
 
 // Rows that keep more tokens than pass 2 holds, by mass alone: every row in parts, all workgroups of the launch
-// taking parts in turn.  Pass 3 sums the weights by bins of the logit.  Pass 4 finds the bin in which the mass
-// is reached, sums each group's weights above it and lists the bin's own tokens.
+// taking parts in turn.  Pass 3 sums the weights, coarsely, by bins of the logit.  Pass 4 finds the bin in which the
+// mass is reached, sums each group's weights above it and lists the bin's own tokens.  (Where the rounding named a
+// bin beside the cut's, pass 5 sees that and leaves the row to pass 6.)
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPartList = 1024;
 
 // Whether rows are shared out: where pass 2 can hold their sub-blocks, and they are long, or many, enough to
@@ -919,7 +1012,7 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_part_kernel(SampleArg
     typedef typename Element<kType>::T T;
     __shared__ Block<kPartThreads> block;
     __shared__ u64 box[kSurvey ? kPartList : kNearBins];      // listed tokens, or the part's bins
-    __shared__ u64 found[2];
+    __shared__ int32_t found;
     __shared__ uint32_t listed, start;
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_of_block();
     const uint32_t rows = s.queued[kShared];
@@ -933,17 +1026,18 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_part_kernel(SampleArg
         const Row r(a, row);
         if (!kSurvey && !r.by_mass) continue;        // min-p alone: no bin to find
         Near* const mine = s.near + row;
-        const Near near{mine->high, mine->steps, mine->top, 0, 0};
+        const Near near{mine->high, mine->steps, mine->top, 0, 0.0, Mass{0, 0}};
         u64* const bins = s.bins + row * kNearBins;
-        const Units weight_of(Weights(value_of(near.top), r.t), bits, near.top);
+        const Reals weight_of(Weights(value_of(near.top), r.t), near.top);
         const int64_t groups = z.groups();
         const int32_t from = (int32_t)(part * groups / parts), to = (int32_t)((part + 1) * groups / parts);
         if constexpr (!kSurvey) {
             for (int b = tid; b < kNearBins; b += kPartThreads) box[b] = 0;
             __syncthreads();
+            const Coarse coarse(bits);
             over_groups(
-                z, from + wave, to, kPartWaves, [&](float x, int64_t) { atomicAdd(&box[near.bin(x)], weight_of(x)); },
-                [](int32_t) {});
+                z, from + wave, to, kPartWaves,
+                [&](float x, int64_t) { atomicAdd(&box[near.bin(x)], coarse(weight_of(x))); }, [](int32_t) {});
             __syncthreads();
             for (int b = tid; b < kNearBins; b += kPartThreads)
                 if (box[b] != 0) atomicAdd(&bins[b], box[b]);
@@ -958,42 +1052,42 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_part_kernel(SampleArg
 #pragma unroll
                 for (int c = 0; c < kEach; ++c) sum += each[c] = bins[kNearBins - 1 - (tid * kEach + c)];
                 u64 have = block.before(sum, block.u, &total);
-                const u64 want = max((u64)1, share(r.p, total, true));
+                const u64 want = max((u64)1, (u64)share(r.p, total, true));
                 if (have < want && have + sum >= want) {
 #pragma unroll
                     for (int c = 0; c < kEach; ++c) {
-                        if (have < want && have + each[c] >= want) {
-                            found[0] = (u64)(kNearBins - 1 - (tid * kEach + c));
-                            found[1] = want - have;
-                        }
+                        if (have < want && have + each[c] >= want) found = kNearBins - 1 - (tid * kEach + c);
                         have += each[c];
                     }
                 }
                 __syncthreads();
-                bin = (int32_t)found[0];
-                if (part == 0 && tid == 0) mine->rest = found[1];
+                bin = found;
             } else {
                 __syncthreads();
             }
-            const u64 floor = r.by_floor ? (u64)ceil((double)r.m * (double)(1ull << bits)) : 0;
-            u64 above = 0;
+            const double floor = r.by_floor ? (double)r.m : 0.0;
+            double above = 0.0, kept = 0.0;              // `kept`: of those above, what min-p keeps
+            Mass all_above{0, 0};
             over_groups(
                 z, from + wave, to, kPartWaves,
                 [&](float x, int64_t at) {
                     const int32_t b = (int32_t)near.bin(x);
                     if (b > bin) {
-                        const u64 y = weight_of(x);
-                        above += y >= floor ? y : 0;
+                        const double y = weight_of(x);
+                        above += y;
+                        if (r.by_floor) kept += y >= floor ? y : 0.0;
                     } else if (b == bin) {
                         const uint32_t i = atomicAdd(&listed, 1u);
                         if (i < kPartList) box[i] = (u64)at << 32 | key_of(x);
                     }
                 },
                 [&](int32_t g) {
-                    for (int x = 32; x > 0; x >>= 1) above += (u64)__shfl_xor((long long)above, x);
-                    if (lane == 0) ((u64*)s.sums)[row * s.groups + g] = above;
-                    above = 0;
+                    if (r.by_mass) all_above += mass_of(above = wave_sum(above));
+                    if (r.by_floor) above = wave_sum(kept);
+                    if (lane == 0) s.sums[row * s.groups + g] = above;
+                    above = kept = 0.0;
                 });
+            if (r.by_mass && lane == 0) add_to(&mine->above.high, &mine->above.low, all_above);
             __syncthreads();
             // more than there is room for: a number that no list has
             if (tid == 0 && listed > 0) start = atomicAdd(&mine->collected, listed <= kPartList ? listed : 1u << 24);
@@ -1015,10 +1109,13 @@ constexpr int kFinishList = 1024, kFinishEach = kFinishList / kPartThreads;
 static_assert(kMostSubs / kSubs <= kPartThreads, "a thread a group");
 
 template <int kType>
-__global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleArgs a, Stats s, int bits) {
+__global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleArgs a, Stats s) {
     typedef typename Element<kType>::T T;
     __shared__ Block<kPartThreads> block;
-    __shared__ u64 order[kFinishList], ranked[kFinishList], kept_in[kPartThreads], pick[2];
+    __shared__ u64 order[kFinishList];
+    __shared__ Mass ranked[kFinishList], kept_in[kPartThreads];
+    __shared__ u128 pick_run;
+    __shared__ int32_t pick;
     const int tid = threadIdx.x;
     const uint32_t rows = s.queued[kShared];
     for (uint32_t q = blockIdx.x; q < rows; q += gridDim.x) {
@@ -1034,14 +1131,14 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleA
         }
         const Grid<T> z(a, row);
         const Row r(a, row);
-        const Units weight_of(Weights(value_of(near.top), r.t), bits, near.top);
-        const u64 floor = r.by_floor ? (u64)ceil((double)r.m * (double)(1ull << bits)) : 0;
-        const auto kept_weight = [&](float x) -> u64 {
-            const u64 y = weight_of(x);
-            return y >= floor ? y : 0;
+        const Reals weight_of(Weights(value_of(near.top), r.t), near.top);
+        const double floor = r.by_floor ? (double)r.m : 0.0;
+        const auto kept_weight = [&](float x) -> Mass {
+            const double y = weight_of(x);
+            return y >= floor ? mass_of(y) : Mass{0, 0};
         };
         const int32_t groups = z.groups();
-        kept_in[tid] = tid < groups ? ((const u64*)s.sums)[row * s.groups + tid] : 0;
+        kept_in[tid] = mass_of(tid < groups ? s.sums[row * s.groups + tid] : 0.0);
         uint32_t cut = 0, ties = 0;          // kept: greater keys, and the first `ties` tokens that have it
         const u64* const list = (const u64*)(s.subs + row * s.groups * kSubs);
         uint32_t key[kFinishEach], place[kFinishEach];
@@ -1053,7 +1150,7 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleA
                 key[c] = (uint32_t)x;
                 place[c] = (uint32_t)(x >> 32);
                 order[i] = i < n ? (u64)key[c] << 32 | (uint32_t)~place[c] : 0;
-                ranked[i] = 0;
+                ranked[i] = Mass{0, 0};
             }
             __syncthreads();
             uint32_t rank[kFinishEach];
@@ -1066,13 +1163,20 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleA
 #pragma unroll
                     for (int e = 0; e < 16; ++e) rank[c] += order[i + e] > own;
                 }
-                if (c * kPartThreads + tid < n) ranked[rank[c]] = weight_of(value_of(key[c]));
+                if (c * kPartThreads + tid < n) ranked[rank[c]] = mass_of(weight_of(value_of(key[c])));
             }
             __syncthreads();
-            u64 of[kFinishEach], sum = 0, whole;
+            Mass of[kFinishEach], sum{0, 0}, whole;
 #pragma unroll
             for (int c = 0; c < kFinishEach; ++c) sum += of[c] = ranked[tid * kFinishEach + c];
-            u64 before = block.before(sum, block.u, &whole);
+            Mass before = block.before(sum, block.m, &whole);
+            // what is wanted of the list: some of it, and no more than it has, or the cut lies in another bin
+            const u128 want = units_of((double)r.p * near.all), above = near.above.value();
+            if (want <= above || want - above > whole.value()) {
+                if (tid == 0) enqueue(s, kAlone, row);
+                continue;
+            }
+            const u128 rest = want - above;
 #pragma unroll
             for (int c = 0; c < kFinishEach; ++c) {
                 ranked[tid * kFinishEach + c] = before;
@@ -1083,10 +1187,11 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleA
             bool kept[kFinishEach];
 #pragma unroll
             for (int c = 0; c < kFinishEach; ++c) {
-                kept[c] = c * kPartThreads + tid < n && ranked[rank[c]] < near.rest;
+                kept[c] = c * kPartThreads + tid < n && ranked[rank[c]].value() < rest;
                 if (kept[c]) {
                     least = min(least, key[c]);
-                    atomicAdd(&kept_in[place[c] / kGroup], kept_weight(value_of(key[c])));
+                    Mass* const to = &kept_in[place[c] / kGroup];
+                    add_to(&to->high, &to->low, kept_weight(value_of(key[c])));
                 }
             }
             cut = block.min(least);
@@ -1095,16 +1200,17 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleA
             ties = block.count(same);
         }
         __syncthreads();
-        const u64 mine = kept_in[tid];
-        u64 total, all;
-        const u64 before = block.before(mine, block.u, &all), target = share(u, all, false);
-        if (mine > 0 && before <= target && before + mine > target) {
-            pick[0] = (u64)tid;
-            pick[1] = before;
+        const Mass mine = kept_in[tid];
+        Mass sum_of_all;
+        const u128 before = block.before(mine, block.m, &sum_of_all).value(), all = sum_of_all.value();
+        const u128 target = share(u, all, false);
+        if (before <= target && before + mine.value() > target) {
+            pick = tid;
+            pick_run = before;
         }
         __syncthreads();
-        const int64_t from = (int64_t)pick[0] * kGroup;
-        u64 run = pick[1];
+        const int64_t from = (int64_t)pick * kGroup;
+        const double rest_of = real_of(target - pick_run);         // that the group's running sum has to exceed
         uint32_t seen = 0;                   // tokens that have the cut's key before the group's
         if (r.by_mass) {
 #pragma unroll
@@ -1127,20 +1233,30 @@ __global__ __launch_bounds__(kPartThreads) void asd_sample_finish_kernel(SampleA
             tied += r.by_mass && k[e] == cut;
         }
         seen += block.before(tied, (uint32_t*)block.u, &all_tied);
-        u64 y[kEach], sum = 0;
+        double y[kEach], sum = 0.0, total;
 #pragma unroll
         for (int e = 0; e < kEach; ++e) {
             const bool kept = k[e] > cut || (r.by_mass && k[e] == cut && seen++ < ties);
-            sum += y[e] = kept ? kept_weight(x[e]) : 0;
+            const double weight = kept ? weight_of.w(x[e]) : 0.0;      // (-inf: none at all)
+            sum += y[e] = weight >= floor ? weight : 0.0;
         }
-        run += block.before(sum, block.u, &total);
+        // the first thread whose tokens pass it; rounding may leave none: the last with a weight
+        double run = block.before(sum, block.d, &total);
+        uint32_t passes = block.min(sum > 0.0 && run + sum > rest_of ? (uint32_t)tid : ~0u);
+        if (passes == ~0u) passes = block.max(sum > 0.0 ? (uint32_t)tid : 0u);
+        if ((uint32_t)tid == passes) {
+            int at = 0;
+            double weight = 0.0;
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            if (run <= target && run + y[e] > target) {
-                a.out_token[row] = (int32_t)(from + tid * kEach + e - z.shift);
-                if (a.out_prob) a.out_prob[row] = (float)((double)y[e] / (double)all);
+            for (int e = 0; e < kEach; ++e) {
+                if (y[e] > 0.0 && !(weight > 0.0 && run > rest_of)) {
+                    at = e;
+                    weight = y[e];
+                }
+                run += y[e];
             }
-            run += y[e];
+            a.out_token[row] = (int32_t)(from + tid * kEach + at - z.shift);
+            if (a.out_prob) a.out_prob[row] = (float)(weight / real_of(all));
         }
     }
 }
@@ -1158,13 +1274,15 @@ template <int kType>
 __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, int bits, int64_t row) {
     typedef typename Element<kType>::T T;
     __shared__ Block<kFlatThreads> block;
-    __shared__ u64 bin_weight[kBins];
+    __shared__ u64 bin_high[kBins], bin_low[kBins];          // Mass by bin
     __shared__ uint32_t bin_count[kBins];
     __shared__ uint32_t key[kCollected], place[kCollected];
-    __shared__ u64 span_sum[kSpans];
+    __shared__ Mass span_sum[kSpans];
     __shared__ uint32_t span_ties[kSpans];
     __shared__ uint32_t collected;
-    __shared__ u64 pick[4];
+    __shared__ u128 pick[2];
+    __shared__ u64 pick_ties;
+    __shared__ Mass in_all;                                  // that a reading of the row summed up
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_of_block();
     const Grid<T> z(a, row);
     const Row r(a, row);
@@ -1174,34 +1292,40 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
     for (int32_t g = tid; g < groups; g += kFlatThreads) top = max(top, s.tops[row * s.groups + g]);
     top = block.max(top);
     const Weights w(value_of(top), r.t);
-    const double unit = (double)(1ull << bits);
-    const Units weight_of(w, bits, top);
-    // min-p in units: a weight counts from there on.  (Rounded up; the greatest token's always does.)
-    const u64 floor = r.by_floor ? (u64)ceil((double)r.m * unit) : 0;
-    const auto kept_weight = [&](float z) -> u64 {
-        const u64 x = weight_of(z);
-        return x >= floor ? x : 0;
+    const Reals real(w, top);
+    const double floor = r.by_floor ? (double)r.m : 0.0;
+    const auto weight_of = [&](float z) -> Mass { return mass_of(real(z)); };
+    const auto kept_weight = [&](float z) -> Mass {
+        const double x = real(z);
+        return x >= floor ? mass_of(x) : Mass{0, 0};
     };
 
     const auto over = [&](auto&& f, auto&& end) { over_groups(z, wave, groups, kFlatWaves, f, end); };
     const auto nothing = [](int32_t) {};
 
-    // What every span holds: the weights of the tokens whose order exceeds `at_order`, and, of those that have
-    // it, the tokens themselves (key and place), or, where the order is the whole key, how many there are.
+    // What every span holds: the weights of the tokens whose order exceeds `at_order`, less what min-p drops (all of
+    // them in in_all), and, of those that have it, the tokens themselves (key and place), or, where the order is
+    // the whole key, how many there are.
     const auto survey = [&](auto&& order, uint32_t at_order, bool whole_key, uint32_t limit) {
         for (int i = tid; i < kSpans; i += kFlatThreads) {
-            span_sum[i] = 0;
+            span_sum[i] = Mass{0, 0};
             span_ties[i] = 0;
         }
-        if (tid == 0) collected = 0;
+        if (tid == 0) {
+            collected = 0;
+            in_all = Mass{0, 0};
+        }
         __syncthreads();
-        u64 mine = 0;
+        double above = 0.0, kept = 0.0;              // `kept`: of those above, what min-p keeps
+        Mass of_wave{0, 0};
         uint32_t same = 0;
         over(
             [&](float x, int64_t at) {
                 const uint32_t b = order(x);
                 if (b > at_order) {
-                    mine += kept_weight(x);
+                    const double y = real(x);
+                    above += y;
+                    if (r.by_floor) kept += y >= floor ? y : 0.0;
                 } else if (b == at_order) {
                     const uint32_t k = key_of(x);
                     if (k < limit) return;
@@ -1217,50 +1341,55 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
                 }
             },
             [&](int32_t g) {
-                for (int x = 32; x > 0; x >>= 1) {
-                    mine += (u64)__shfl_xor((long long)mine, x);
-                    same += (uint32_t)__shfl_xor((int)same, x);
-                }
+                above = wave_sum(above);
+                of_wave += mass_of(above);
+                if (r.by_floor) above = wave_sum(kept);
+                for (int x = 32; whole_key && x > 0; x >>= 1) same += (uint32_t)__shfl_xor((int)same, x);
                 if (lane == 0) {
-                    atomicAdd(&span_sum[g / per_span], mine);
-                    atomicAdd(&span_ties[g / per_span], same);
+                    Mass* const span = &span_sum[g / per_span];
+                    add_to(&span->high, &span->low, mass_of(above));
+                    if (whole_key) atomicAdd(&span_ties[g / per_span], same);
                 }
-                mine = 0;
+                above = kept = 0.0;
                 same = 0;
             });
+        if (lane == 0) add_to(&in_all.high, &in_all.low, of_wave);
         __syncthreads();
     };
     const auto clear_bins = [&]() {
         for (int b = tid; b < kBins; b += kFlatThreads) {
-            bin_weight[b] = 0;
+            bin_high[b] = bin_low[b] = 0;
             bin_count[b] = 0;
         }
+        if (tid == 0) in_all = Mass{0, 0};
         __syncthreads();
     };
-    // The bin in which `want` is reached, from the last one down, and what is still wanted of it: four bins a thread.
-    const auto find_bin = [&](bool weights, u64* want) -> uint32_t {
+    // The bin in which `want` is reached, from the last one down, and what is still wanted of it: eight bins a thread.
+    enum { kCounts, kCoarsely, kFinely };
+    const auto find_bin = [&](int kind, u128* want) -> uint32_t {
         constexpr int kEach = kBins / kFlatThreads;
-        u64 each[kEach], mine = 0, total;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
+        const auto of = [&](int i) {
             const int b = kBins - 1 - (kEach * tid + i);
-            each[i] = weights ? bin_weight[b] : bin_count[b];
-            mine += each[i];
-        }
-        u64 have = block.before(mine, block.u, &total);
+            return kind == kFinely ? Mass{bin_high[b], bin_low[b]} : Mass{0, kind == kCounts ? bin_count[b] : bin_high[b]};
+        };
+        Mass mine{0, 0}, total;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) mine += of(i);
+        u128 have = block.before(mine, block.m, &total).value();
         if (tid == 0) {
             pick[0] = 0;
             pick[1] = *want;
         }
         __syncthreads();
-        if (have < *want && have + mine >= *want) {
+        if (have < *want && have + mine.value() >= *want) {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
-                if (have < *want && have + each[i] >= *want) {
-                    pick[0] = (u64)(kBins - 1 - (kEach * tid + i));
+                const u128 upto = have + of(i).value();
+                if (have < *want && upto >= *want) {
+                    pick[0] = (u128)(kBins - 1 - (kEach * tid + i));
                     pick[1] = *want - have;
                 }
-                have += each[i];
+                have = upto;
             }
         }
         __syncthreads();
@@ -1269,7 +1398,6 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
         __syncthreads();
         return bin;
     };
-
     // Keys above `cut` are kept, and the first `ties` tokens that have it; stage 0 cuts by count, stage 1 by
     // mass among what stage 0 left.
     uint32_t cut = 0;
@@ -1285,46 +1413,78 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
         if (!(stage == 0 ? r.by_count : r.by_mass)) continue;
         const bool by_weight = stage == 1;
         const uint32_t limit = cut;
-        const u64 limit_ties = ties, limit_weight = limit ? weight_of(value_of(limit)) : 0;
-        const u64 limit_mass = by_weight && limit != 0 ? limit_ties * limit_weight : 0;
-        const auto worth = [&](uint32_t k) -> u64 {      // of a token beyond the limit's
-            return !by_weight ? 1 : k > limit ? weight_of(value_of(k)) : 0;
+        const u64 limit_ties = ties;
+        const Mass limit_weight = limit ? weight_of(value_of(limit)) : Mass{0, 0};
+        const Mass limit_mass = by_weight && limit != 0 ? limit_weight * limit_ties : Mass{0, 0};
+        const bool limited = limit_mass.value() != 0;
+        const auto worth = [&](uint32_t k) -> Mass {     // of a token beyond the limit's
+            return !by_weight ? Mass{0, 1} : k > limit ? weight_of(value_of(k)) : Mass{0, 0};
         };
-        u64 want = (u64)r.k;
+        u128 want = (u128)(uint32_t)r.k;
         bool listed = false, limit_in = false;        // a list, and the limit's tokens in it
         if (top < kKeyInf) {
             clear_bins();
+            const Coarse coarse(bits);
+            double part = 0.0;
+            Mass of_wave{0, 0};
             over(
                 [&](float x, int64_t) {
                     const uint32_t b = near_top(x);
-                    if (!by_weight) atomicAdd(&bin_count[b], 1u);
-                    else if (limit == 0 || key_of(x) > limit) atomicAdd(&bin_weight[b], weight_of(x));
+                    if (!by_weight) {
+                        atomicAdd(&bin_count[b], 1u);
+                    } else if (limit == 0 || key_of(x) > limit) {
+                        const double y = real(x);
+                        atomicAdd(&bin_high[b], coarse(y));
+                        part += y;
+                    }
                 },
-                nothing);
+                [&](int32_t) {
+                    if (!by_weight) return;
+                    of_wave += mass_of(wave_sum(part));
+                    part = 0.0;
+                });
+            if (lane == 0) add_to(&in_all.high, &in_all.low, of_wave);
             __syncthreads();
             // of the tokens at the limit only those count that stage 0 kept
-            if (limit_mass != 0 && tid == 0) bin_weight[near_top(value_of(limit))] += limit_mass;
+            if (limited && tid == 0) bin_high[near_top(value_of(limit))] += coarse(real(value_of(limit))) * limit_ties;
             __syncthreads();
+            u128 rest = want;
             if (by_weight) {
-                u64 mine = 0;
-                for (int b = tid; b < kBins; b += kFlatThreads) mine += bin_weight[b];
-                want = max((u64)1, share(r.p, block.sum(mine), true));
+                want = max((u128)1, share(r.p, (in_all + limit_mass).value(), true));
+                Mass mine{0, 0};
+                for (int b = tid; b < kBins; b += kFlatThreads) mine.low += bin_high[b];
+                rest = max((u128)1, share(r.p, block.sum(mine).value(), true));
             }
-            u64 rest = want;
-            const uint32_t bin = find_bin(by_weight, &rest);
+            const uint32_t bin = find_bin(by_weight ? kCoarsely : kCounts, &rest);
+            const u64 in_bin = bin_high[bin];
             survey(near_top, bin, false, limit);
             listed = collected <= (uint32_t)kCollected;
+            limit_in = limited && near_top(value_of(limit)) == bin;
+            if (listed && by_weight) {
+                // Some of the listed has to be wanted, and no more than there is, or the cut lies in another bin.
+                // (Each of a bin's coarse weights is half a unit off at most.)
+                const u128 above = in_all.value();
+                listed = want > above;
+                rest = want - above;
+                if (listed && rest > (u128)(in_bin - min(in_bin, (u64)collected)) << (64 - bits)) {
+                    Mass mine{0, 0};
+                    for (int i = tid; i < (int)collected; i += kFlatThreads) mine += worth(key[i]);
+                    Mass of_list = block.sum(mine);
+                    if (limit_in) of_list += limit_mass;
+                    listed = rest <= of_list.value();
+                }
+            }
             if (listed) want = rest;
-            limit_in = limit_mass != 0 && near_top(value_of(limit)) == bin;
         }
         uint32_t prefix = 0;            // of the cut's key, from bit `shift` up
         int shift = 32;
         if (!listed) {
-            // More tokens in one bin than the list holds: by the keys' bits.
+            // More tokens in one bin than the list holds, or another bin: by the keys' bits.
+            __syncthreads();
             if (by_weight && !(top < kKeyInf)) {
-                u64 mine = 0;
-                over([&](float x, int64_t) { mine += key_of(x) > limit ? weight_of(x) : 0; }, nothing);
-                want = max((u64)1, share(r.p, block.sum(mine) + limit_mass, true));
+                Mass mine{0, 0};
+                over([&](float x, int64_t) { if (key_of(x) > limit) mine += weight_of(x); }, nothing);
+                want = max((u128)1, share(r.p, (block.sum(mine) + limit_mass).value(), true));
             }
             u64 in_bin = ~0ull;
             while (shift > 0 && in_bin > (u64)kCollected) {
@@ -1336,15 +1496,17 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
                         const uint32_t k = key_of(x);
                         if (k < limit || (shift < 32 && k >> shift != prefix)) return;
                         const uint32_t b = k >> low & mask;
-                        if (by_weight && k > limit) atomicAdd(&bin_weight[b], weight_of(x));
+                        if (by_weight && k > limit) add_to(&bin_high[b], &bin_low[b], weight_of(x));
                         atomicAdd(&bin_count[b], 1u);
                     },
                     nothing);
                 __syncthreads();
-                if (limit_mass != 0 && (shift == 32 || limit >> shift == prefix) && tid == 0)
-                    bin_weight[limit >> low & mask] += limit_mass;
+                if (limited && (shift == 32 || limit >> shift == prefix) && tid == 0) {
+                    bin_high[limit >> low & mask] += limit_mass.high;
+                    bin_low[limit >> low & mask] += limit_mass.low;
+                }
                 __syncthreads();
-                const uint32_t bin = find_bin(by_weight, &want);
+                const uint32_t bin = find_bin(by_weight ? kFinely : kCounts, &want);
                 in_bin = bin_count[bin];
                 prefix = (shift == 32 ? 0u : prefix << (shift - low)) | bin;
                 shift = low;
@@ -1352,7 +1514,7 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
             }
             survey([&](float x) { return key_of(x) >> shift; }, prefix, shift == 0, limit);
             listed = shift > 0;
-            limit_in = limit_mass != 0 && listed && limit >> shift == prefix;
+            limit_in = limited && listed && limit >> shift == prefix;
         }
         if (listed) {
             // the cut among the listed tokens
@@ -1362,12 +1524,12 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
                 // tokens in that order.  Those that have the limit's key come last, and the first
                 // limit_ties of them count.
                 const uint32_t k = tid < n ? key[tid] : 0;
-                u64* const order = bin_weight;               // done with
-                u64* const ranked = bin_weight + kFlatThreads;
-                u64* const sums = ranked + kFlatThreads;
+                u64* const order = bin_high;                 // done with
+                Mass* const ranked = (Mass*)bin_low;
+                Mass* const sums = ranked + kFlatThreads;
                 const u64 own = tid < n ? (u64)k << 32 | (uint32_t)~place[tid] : 0;
                 order[tid] = own;
-                ranked[tid] = 0;
+                ranked[tid] = Mass{0, 0};
                 __syncthreads();
                 uint32_t rank = 0;
                 if (wave * 64 < n) {
@@ -1376,48 +1538,57 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
                         for (int e = 0; e < 16; ++e) rank += order[i + e] > own;
                     }
                 }
-                u64 before = rank;
+                u128 before = rank;
                 bool counts = true;
                 if (by_weight) {
                     const uint32_t more = block.count(k > limit);
                     counts = k > limit || rank - more < limit_ties;
-                    if (tid < n) ranked[rank] = k > limit ? weight_of(value_of(k)) : counts ? limit_weight : 0;
+                    if (tid < n) ranked[rank] = k > limit ? weight_of(value_of(k)) : counts ? limit_weight : Mass{0, 0};
                     __syncthreads();
-                    u64 all;
-                    sums[tid] = block.before(ranked[tid], block.u, &all);
+                    Mass all;
+                    sums[tid] = block.before(ranked[tid], block.m, &all);
                     __syncthreads();
-                    if (tid < n) before = sums[rank];
+                    if (tid < n) before = sums[rank].value();
                 }
                 const bool kept = tid < n && before < want && counts;
                 prefix = block.min(kept ? k : ~0u);
-                want = block.count(kept && k == prefix);
+                ties = block.count(kept && k == prefix);
                 cut = prefix;
-                ties = want;
             } else {
-                prefix = shift == 32 ? 0u : prefix;
-                while (shift > 0) {
-                    const uint32_t trial = (prefix << 1 | 1u) << (shift - 1);
-                    u64 mine = 0;
-                    for (int i = tid; i < n; i += kFlatThreads)
-                        if (key[i] >= trial) mine += worth(key[i]);
-                    u64 reach = block.sum(mine);
-                    if (limit_in && trial <= limit) reach += limit_mass;
-                    prefix = prefix << 1 | (reach >= want ? 1u : 0u);
-                    --shift;
+                // The greatest of their keys that is reached, by those bits in which they differ.
+                uint32_t differ = 0;
+                for (int i = tid; i < n; i += kFlatThreads) differ |= key[i] ^ key[0];
+                differ = block.any(differ);
+                prefix = key[0] & ~differ;
+                for (; differ != 0; differ &= ~(1u << (31 - __builtin_clz(differ)))) {
+                    const uint32_t trial = prefix | 1u << (31 - __builtin_clz(differ));
+                    bool reached;
+                    if (by_weight) {
+                        Mass mine{0, 0};
+                        for (int i = tid; i < n; i += kFlatThreads)
+                            if (key[i] >= trial) mine += worth(key[i]);
+                        Mass reach = block.sum(mine);
+                        if (limit_in && trial <= limit) reach += limit_mass;
+                        reached = reach.value() >= want;
+                    } else {
+                        uint32_t mine = 0;
+                        for (int i = tid; i < n; i += kFlatThreads) mine += key[i] >= trial;
+                        reached = block.count(mine) >= want;
+                    }
+                    if (reached) prefix = trial;
                 }
-                u64 mine = 0;
+                Mass mine{0, 0};
                 for (int i = tid; i < n; i += kFlatThreads)
                     if (key[i] > prefix) mine += worth(key[i]);
-                want -= min(want, block.sum(mine));
-                const u64 one = by_weight ? weight_of(value_of(prefix)) : 1;
-                const u64 m = max((u64)1, one > 0 ? (want + one - 1) / one : 1);
+                want -= min(want, block.sum(mine).value());
+                const u64 m = ties_for(want, by_weight ? weight_of(value_of(prefix)).value() : 1);
                 ties = by_weight && prefix == limit ? min(m, limit_ties) : m;
                 cut = prefix;
             }
             for (int i = tid; i < n; i += kFlatThreads) {
                 const int32_t span = (int32_t)(place[i] / (uint32_t)kGroup) / per_span;
                 if (key[i] > cut) {
-                    atomicAdd(&span_sum[span], kept_weight(value_of(key[i])));
+                    add_to(&span_sum[span].high, &span_sum[span].low, kept_weight(value_of(key[i])));
                 } else if (key[i] == cut) {
                     atomicAdd(&span_ties[span], 1u);
                 }
@@ -1425,19 +1596,19 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
             __syncthreads();
         } else {
             cut = prefix;
-            const u64 one = by_weight ? weight_of(value_of(cut)) : 1;
-            const u64 m = max((u64)1, one > 0 ? (want + one - 1) / one : 1);
+            const u64 m = ties_for(want, by_weight ? weight_of(value_of(cut)).value() : 1);
             ties = by_weight && cut == limit ? min(m, limit_ties) : m;
         }
     }
     if (!r.by_count && !r.by_mass) survey([](float x) { return key_of(x); }, 0, true, 0);
-    const u64 cut_weight = cut != 0 ? kept_weight(value_of(cut)) : 0;
+    const Mass cut_weight = cut != 0 ? kept_weight(value_of(cut)) : Mass{0, 0};
     const u64 here = tid < spans ? span_ties[tid] : 0;
-    u64 total;
-    const u64 ties_before = block.before(here, block.u, &total);
+    u64 all_ties;
+    const u64 ties_before = block.before(here, block.u, &all_ties);
     const u64 kept_ties = ties_before < ties ? min(here, ties - ties_before) : 0;
-    const u64 sum = tid < spans ? span_sum[tid] + kept_ties * cut_weight : 0;
-    const u64 before = block.before(sum, block.u, &total);
+    const Mass sum = tid < spans ? span_sum[tid] + cut_weight * kept_ties : Mass{0, 0};
+    Mass total;
+    const u128 before = block.before(sum, block.m, &total).value(), all = total.value();
     const float u = inside_unit(a.uniform[row]);
     if (u == 0.0f) {
         // the first kept token, which may weigh less than a unit
@@ -1446,45 +1617,72 @@ __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, in
         over(
             [&](float x, int64_t at) {
                 if (key_of(x) < cut || first != ~0u) return;
-                const double real = w(x);
-                if (real > 0.0 && weight_of(x) >= floor) {
+                const double y = w(x);
+                if (y > 0.0 && y >= floor) {
                     first = (uint32_t)at;
-                    weight = real;
+                    weight = y;
                 }
             },
             nothing);
         const uint32_t place = block.min(first);
         if (first == place) {
             a.out_token[row] = (int32_t)(place - (uint32_t)z.shift);
-            if (a.out_prob) a.out_prob[row] = (float)(weight * unit / (double)total);
+            if (a.out_prob) a.out_prob[row] = (float)(weight / real_of(all));
         }
         return;
     }
-    const u64 all_kept = total, target = share(u, total, false);     // the running sum has to exceed it
-    if (sum > 0 && before <= target && before + sum > target) {
-        pick[0] = (u64)tid;
+    const u128 target = share(u, all, false);            // the running sum has to exceed it
+    if (before <= target && before + sum.value() > target) {
+        pick[0] = (u128)tid;
         pick[1] = before;
-        pick[2] = ties_before;
+        pick_ties = ties_before;
     }
     __syncthreads();
-    // the span's tokens in order
-    u64 run = pick[1], seen = pick[2];
+    // The span's tokens in order, two to a thread, up to the first at which the running sum passes the rest; rounding
+    // may leave none: the last with a weight.
+    const double rest = real_of(target - pick[1]);
+    double run = 0.0, weight = 0.0, part;
+    u64 seen = pick_ties;
+    uint32_t passes = ~0u, last = 0;
     const int64_t from = (int64_t)pick[0] * per_span * kGroup;
     const int64_t to = min(from + (int64_t)per_span * kGroup, z.vocab + z.shift);
-    for (int64_t at = from + tid; at - tid < to && run <= target; at += kFlatThreads) {
-        const bool in = at < to && z.has(at);
-        const float x = in ? z(at) : -INFINITY;
-        const uint32_t k = in ? key_of(x) : 0;
-        u64 tied;
-        const u64 rank = seen + block.before((u64)(in && k == cut), block.u, &tied);
-        const u64 y = in && (k > cut || (k == cut && rank < ties)) ? kept_weight(x) : 0;
-        const u64 upto = run + block.before(y, block.u, &total);
-        if (upto <= target && upto + y > target) {
-            a.out_token[row] = (int32_t)(at - z.shift);
-            if (a.out_prob) a.out_prob[row] = (float)((double)y / (double)all_kept);
+    for (int64_t first = from; first < to && passes == ~0u; first += 2 * kFlatThreads) {
+        const int64_t at = first + 2 * tid;
+        float x[2];
+        uint32_t k[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const bool in = at + e < to && z.has(at + e);
+            x[e] = in ? z(at + e) : -INFINITY;
+            k[e] = in ? key_of(x[e]) : 0;
         }
-        run += total;
+        u64 tied;
+        u64 rank = seen + block.before((u64)(k[0] == cut) + (u64)(k[1] == cut), block.u, &tied);
+        double y[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            y[e] = k[e] > cut || (k[e] != 0 && k[e] == cut && rank++ < ties) ? w(x[e]) : 0.0;
+            if (y[e] < floor) y[e] = 0.0;
+        }
+        double upto = run + block.before(y[0] + y[1], block.d, &part);
+        bool mine = false;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            upto += y[e];
+            if (y[e] > 0.0 && !mine) {
+                last = (uint32_t)(at + e);
+                weight = y[e];
+                mine = upto > rest;
+            }
+        }
+        passes = block.min(mine ? last : ~0u);
+        run += part;
         seen += tied;
+    }
+    const uint32_t drawn = passes != ~0u ? passes : block.max(last);
+    if (last == drawn && weight > 0.0) {
+        a.out_token[row] = (int32_t)(drawn - (uint32_t)z.shift);
+        if (a.out_prob) a.out_prob[row] = (float)(weight / real_of(all));
     }
 }
 
@@ -1516,7 +1714,7 @@ hipError_t sample(const SampleArgs& a, const Stats& s, int32_t per_wave, int bit
         asd_sample_part_kernel<kType, true><<<grid, kPartThreads, 0, stream>>>(a, s, bits);
         if ((err = hipGetLastError()) != hipSuccess) return err;
         asd_sample_finish_kernel<kType>
-            <<<(unsigned)(a.rows < grid ? a.rows : grid), kPartThreads, 0, stream>>>(a, s, bits);
+            <<<(unsigned)(a.rows < grid ? a.rows : grid), kPartThreads, 0, stream>>>(a, s);
         if ((err = hipGetLastError()) != hipSuccess) return err;
     }
     asd_sample_flat_kernel<kType>
