@@ -42,11 +42,12 @@ def log(*a):
 
 
 def kernel_source_hash() -> str:
-    """Hash of the library's sources with comments and whitespace removed (the
-    hash the build embeds in the library), so that an edit to a comment does
-    not detach the counter profiles measured on the same code."""
-    from paper_2608_03447_amd.build import source_hash
-    return source_hash()
+    """Hash of the sources that decide what the verifier's kernels do, with
+    comments and whitespace removed, so that neither an edit to a comment nor
+    one to the other operators detaches the counter profiles measured on the
+    same code."""
+    from paper_2608_03447_amd.build import VERIFIER_SOURCES, source_hash
+    return source_hash(VERIFIER_SOURCES)
 
 
 def algorithmic_bytes(w) -> int:

@@ -29,6 +29,8 @@ SOURCES = [os.path.join(CSRC, "asd_api.cpp"), os.path.join(CSRC, "asd_kernels.hi
 # code goes into the library.
 HASHED_SOURCES = [os.path.join(CSRC, "asd_kernels.hip"), os.path.join(CSRC, "asd_plan.h"),
                   os.path.join(CSRC, "asd_api.cpp"), os.path.join(ROOT, "include", "asd.h")]
+# Those that decide what the verifier's kernels do: their code, and the plan of their launches.
+VERIFIER_SOURCES = HASHED_SOURCES[:3]
 # The binding's native marshalling (a CPython module over torch's C++ tensors).
 BINDING = os.path.join(HERE, "_asd_binding.so")
 BINDING_SOURCES = [os.path.join(CSRC, "asd_binding.cpp"), os.path.join(ROOT, "include", "asd.h")]
