@@ -23,12 +23,13 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 // find its keys and values in the L2.
 //
 // Bounds and measurements (128-element heads in bfloat16, 32 query heads to 8 key heads unless said):
-//  - single tokens and blocks: the cache's bytes.  64 single tokens over up to 8,192: 216 us, 5.0 TB/s where a
+//  - single tokens and blocks: the cache's bytes.  64 single tokens over up to 8,192: 217 us, 5.0 TB/s where a
 //    plain read reaches 6.9; some 25 us of it are the batch's sharing out, each item's first loads and the
-//    join.  9 rows over 65,000: 74 us for 266 MB, of it the join 11.  One token over 700: 12.2 us, a chain of
+//    join.  9 rows over 65,000: 75 us for 266 MB, of it the join 11.  One token over 700: 12.2 us, a chain of
 //    dependent loads (lengths, page table, keys, values) in two launches.
-//  - trees: the matrix cores and, about as long, the exponentials between the two products.  16 trees of 64
-//    over 16,000, 64 query heads to 8: 839-871 us, 620-640 TFLOP/s where a large matrix product reaches 1,150.
+//  - trees: the vector unit between the two products and the matrix cores, which wait for it.  16 trees of 64
+//    over 16,000, 64 query heads to 8: 830-870 us by the box, 620-650 TFLOP/s where a large matrix product reaches
+//    1,150 to 1,400.  By counters a SIMD's matrix core is busy for 29% of its cycles, its vector unit for about half.
 // A kernel of a workgroup per (row, head), one token at a time, took 13,309, 56,835, 466 and 476,524 us.
 
 constexpr int kAttendThreads = 64 * kAttendWaves;

@@ -89,8 +89,9 @@ template <typename T> __device__ __forceinline__ void put(Piece& x, int e, float
 }
 
 // Heads whose size and rotated part are multiples of 16 elements.  The work is memory's: a row is read and
-// written once, and 4,352 rows of 32 + 2 x 8 heads of 128 (107 MB) take 24.5 us, some 9,200 rows of 64 + 2 x 8
-// (377 MB) 78 us, at the 4.7 TB/s of a large copy (a wavefront per head with 2-byte loads took 99 and 640).
+// written once, and 4,352 rows of 32 + 2 x 8 heads of 128 (107 MB) take 25.3 us, some 9,200 rows of 64 + 2 x 8
+// (377 MB) 77 us, 4.2 and 4.9 TB/s, where a library copy of as many bytes takes 21.6 and 71, an elementwise kernel 20.6
+// and 63.6 (a wavefront per head with 2-byte loads took 99 and 640).
 //
 // A lane holds two 16-byte pieces of a head, those whose elements it turns against each other, and kLanes
 // lanes a head: no element changes its lane, and a head's square sum goes over kLanes lanes.  A step is

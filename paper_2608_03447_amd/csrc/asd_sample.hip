@@ -22,10 +22,10 @@
 //
 // Bounds and measurements: pass 1 is memory's and the binary64 exponentials'; 2,112 rows of 151,936 float32
 // (1.28 GB) take 267 us, 4.8 TB/s.  Pass 2 is latency and, with 1,400 candidates, arithmetic: 12 us for
-// one row of 32,000 with top-k 50, 36 with top-k 1,000 of 129,280, 110 for the 2,112.  Passes 3 and 4 are
-// the exponentials': 74 and 83 us for some 480 flat rows of the 2,112, 9 and 12 for 15 rows of 129,280 in bfloat16;
-// pass 5 26 and 11.  In all 535 us, 85 us for 67 rows of 129,280, 17.7 for one of 32,000 (a bisection over
-// each row by one workgroup took 7,165, 584 and 202).
+// one row of 32,000 with top-k 50, 36 with top-k 1,000 of 129,280, 105 for the 2,112.  Passes 3 and 4 are
+// the exponentials': 69 and 77 us for some 480 flat rows of the 2,112, 9 and 13 for 15 rows of 129,280 in bfloat16;
+// pass 5 22 and 11 to 18.  In all 526-545 us by the box, 84-87 us for 67 rows of 129,280, 16.8 for one of 32,000 (a
+// bisection over each row by one workgroup took 7,165, 584 and 202).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -998,8 +998,8 @@ struct Reals {
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPartList = 1024;
 
 // Whether rows are shared out: where pass 2 can hold their sub-blocks, and they are long, or many, enough to
-// pay for three more launches, 6 us where no row is flat.  One flat row of 32,000 takes 63 us alone, one of
-// 65,000 96 us, one of 151,936 56 us shared out, and so do 16 of 32,000 in 46.
+// pay for three more launches, 6 us where no row is flat.  One flat row of 32,000 takes 67 us alone, one of
+// 65,000 102 us, one of 151,936 56 us shared out, and 16 of 32,000 so 45.
 bool shares_out(int64_t vocab, int64_t rows) {
     return vocab > (rows < 8 ? 65536 : 8192) && vocab + 7 <= (int64_t)kMostSubs * kSub;
 }
@@ -1267,9 +1267,9 @@ constexpr int kFlatThreads = 512, kFlatWaves = kFlatThreads / 64, kBins = 4096, 
 
 // A whole row by one workgroup: histograms of it give the bin that holds the cut, a second reading lists that bin
 // and sums what lies above it.  Each reading is the exponentials' time on one compute unit, some 40 us for
-// 129,280 logits.  Spans (1,024 tokens each up to 2^19 tokens a row) hold what is kept of them.  512
-// threads: 1,024, whose registers did not hold everything, took 61 us against 38 for a call of 8,000 logits with
-// top-p, 83 against 63 for one of 32,000.
+// 129,280 logits.  Spans (1,024 tokens each up to 2^19 tokens a row) hold what is kept of them.  A call of 8,000
+// logits with top-p takes 41 us, one of 32,000 67.  (512 threads: 1,024, whose registers did not hold everything, took
+// 1.6 and 1.3 times as long.)
 template <int kType>
 __device__ __forceinline__ void flat_row(const SampleArgs& a, const Stats& s, int bits, int64_t row) {
     typedef typename Element<kType>::T T;

@@ -175,3 +175,14 @@ def test_cuts_between_any_two_tokens_above_a_far_tail(vocab, rows, calls):
             assert places[where] == int(token[r])
             assert any(fits(k, np.cumsum(k), where, float(prob[r]), float(u[r])) for k in kept), (r, float(p[r]))
     assert cut_short >= 1, "no cut lies within the tail's mass of the next token's"
+
+
+def test_equal_logits_of_a_very_wide_row():
+    """Every running sum is a whole number, so that each token is known."""
+    vocab = (1 << 26) + 3
+    z = torch.zeros((2, vocab), dtype=torch.float16, device=DEV)
+    for kept, args in ((vocab, {}), ((vocab + 1) // 2, dict(top_p=0.5)), (12345677, dict(top_k=12345677)),
+                       (6172839, dict(top_k=12345677, top_p=0.5)), (vocab, dict(min_p=1.0))):
+        for u in ([0.0, 0.5], [0.625, 1 - 2.0 ** -24]):
+            token = asd.asd_sample(z, torch.tensor(u, device=DEV), **args)
+            assert token.tolist() == [int(np.floor(np.longdouble(x) * kept)) for x in u]
